@@ -68,7 +68,7 @@ typedef enum {
 
 typedef enum {
     LVLM_OP_SCORE_TOKENS = 0, LVLM_OP_SELECT_TOPK = 1, LVLM_OP_MERGE_COMPACT = 2,
-    LVLM_OP_KV_COMPRESS = 3, LVLM_OP_DECODE_ATTN = 4, LVLM_OP_PREFILL_ATTN = 5
+    LVLM_OP_KV_COMPRESS = 3, LVLM_OP_DECODE_ATTN = 4, LVLM_OP_PREFILL_ATTN = 5, LVLM_OP_TREE_ATTN = 6
 } lvlm_op;
 
 /* Problem sizes.  Each entry point lists the fields it reads; the others are ignored.
@@ -96,6 +96,22 @@ typedef struct lvlm_dims {
     int64_t hid_stride_b;                        /* hidden[b][row][C], rows packed; default N*C */
     int64_t out_stride_b;                        /* hidden_out[b][row][C]; default (rows after the call)*C */
     int64_t head_stride;                         /* score_head[b][g] rows; default n */
+    int32_t T;           /* rope_append, commit_rows: new rows of a sequence, the longest; tree_attn: drafted tokens, the most */
+    int32_t page;        /* rows of a page of a paged cache: a power of two, at least 16; 0 = the cache is contiguous */
+    int32_t n_pages;     /* pages in a paged cache */
+    int32_t max_pages;   /* entries of a (sequence, KV head) in the page table */
+    int32_t draft_cap;   /* rows allocated per (sequence, KV head) in Kd and Vd */
+    int32_t rot;         /* rope_append: channels that are rotated, a multiple of 16 up to D; 0 = none */
+    int32_t interleaved; /* rope_append: a pair is 0 = (i, i + rot/2), 1 = (2i, 2i + 1) */
+    int32_t n_pos;       /* rope_append: rows of cos_sin */
+    int32_t axes;        /* rope_append: positions of a token, 1 (or 0) or 3 */
+    int32_t sect0;       /* rope_append, axes == 3: the first sect0 frequencies follow axis 0, */
+    int32_t sect1;       /*                         the next sect1 axis 1, the others axis 2 */
+    int32_t count_heads; /* commit_rows: 0 = count is [B], 1 = count is [B][Hkv] */
+    int32_t mask_shared; /* tree_attn: 1 = one mask for all sequences */
+    int64_t new_stride_b, new_stride_n, new_stride_h;  /* k_new,v_new[b][t][g][D]; default packed [B][T][Hkv][D] */
+    int64_t page_stride;                         /* Kc,Vc[page][row][D] of a paged cache, rows packed; default page*D */
+    int64_t draft_stride_b, draft_stride_h;      /* Kd,Vd[b][g][row][D], rows packed; default [B][Hkv][draft_cap][D] */
 } lvlm_dims;
 
 /* Library version string (static storage). */
@@ -298,6 +314,102 @@ lvlm_status lvlm_decode_attn_static(const void* q, void* Kc, void* Vc, int32_t* 
                                     const void* k_new, const void* v_new, float* acc_score,
                                     const lvlm_dims* d, float scale, void* out,
                                     int32_t* dev_status, void* stream);
+
+/*
+ * ---- several new tokens at a time, and paged caches --------------------------------------------------------------
+ *
+ * The three entry points below have no counterpart in the paper.  After lvlm_kv_compress every head has its own
+ * length, but a contiguous cache still occupies cap rows a head; in a PAGED cache the memory that was freed can be used by
+ * others.  And a step that takes a tree of drafted tokens reads the cache once for all of them.
+ *
+ * A cache argument (Kc, Vc, table) is
+ *   contiguous  table == NULL, d->page == 0: [B][Hkv][d->cap][D] with strides d->kv_stride_*
+ *   paged       Kc and Vc are [d->n_pages][d->page][D] (stride d->page_stride), table [B][Hkv][d->max_pages] int32 on the
+ *               device: row j of head (b, g) lies in page table[b][g][j / page] at row j % page.  Its capacity is
+ *               cap = max_pages * page.  Entries behind a head's length are not read.  Heads may share pages that are only read;
+ *               a page that is appended to belongs to one head.
+ * Drafted tokens are kept out of the cache: their keys and values lie in a small contiguous cache of their own,
+ * Kd, Vd [B][Hkv][d->draft_cap][D], filled by lvlm_rope_append (len = NULL); after the verification lvlm_commit_rows appends
+ * the accepted ones to the cache.  A rejected draft leaves nothing to undo.
+ *
+ * In all three, `count` (NULL = d->T everywhere) holds the new rows or drafts of each sequence, at most d->T; what
+ * belongs to the others is neither read nor written.  A count outside [0, T] is taken as 0 and sets LVLM_DEV_BOUNDS.
+ * A head whose len lies outside [0, cap], or an append that does not fit behind it, is skipped: nothing of that head is written,
+ * its length stays, and LVLM_DEV_BOUNDS is set.  A page number outside [0, n_pages) sets it too; an append skips that row,
+ * lvlm_tree_attn takes zeros for the rows of that page.
+ */
+
+/*
+ * Rotary position embedding of new queries and keys, the keys and values appended to a cache on the way.
+ * With c_i = cos_sin[p_i][i], s_i = cos_sin[p_i][rot/2 + i], i < rot/2, a pair (x, y) of channels becomes
+ *     (x c_i - y s_i,  y c_i + x s_i)
+ * in fp32, rounded once; channels from rot on stay as they are.  p_i is the token's position on the axis that frequency i follows.
+ *   q_out[b,t,h]          = rot(q[b,t,h])           q optional [B][T][H][D] (strides d->q_stride_*); q_out [B][T][H][D]
+ *                           packed, or q itself: rotated where it lies.  Any other overlap with q is INVALID_ARG
+ *   K[b,g,len[b,g] + t]   = rot(k_new[b,t,g])       k_new, v_new [B][T][Hkv][D] (strides d->new_stride_*)
+ *   V[b,g,len[b,g] + t]   = v_new[b,t,g]            for t < count[b]
+ *   len_out[b,g]          = len[b,g] + count[b]
+ *   pos        [axes][B][T] int32, positions of the tokens; one outside [0, n_pos) sets LVLM_DEV_BOUNDS and leaves the
+ *              channels that follow it as they are
+ *   cos_sin    [n_pos][rot] fp32; cos_sin and pos are only needed with rot > 0
+ *   len        [B][Hkv] int32, or NULL: all zero (a draft cache)
+ *   len_out    optional [B][Hkv] int32, may be len itself (a second small launch then where T > 1)
+ *   acc_score  optional [B][Hkv][cap] fp32: the new entries become 0, as lvlm_decode_attn starts them
+ *   pos_cache  optional [B][Hkv][cap] int32: the new entries take pos (of axis 0); needs pos
+ * Reads d: B,H,Hkv,D,T,rot,interleaved,n_pos,axes,sect0,sect1,q_stride_*,new_stride_*, and the cache's fields.
+ * Errors: INVALID_ARG (NULL k_new/v_new/Kc/Vc, q without q_out or the reverse, rot > 0 without pos or cos_sin, bad sections, a
+ * table without pages or pages without a table), UNSUPPORTED (D != 128, rot % 16, a page that is no power of two or
+ * below 16), ALIGNMENT.
+ */
+lvlm_status lvlm_rope_append(const void* q, const void* k_new, const void* v_new, const int32_t* pos,
+                             const float* cos_sin, const int32_t* count, void* q_out, void* Kc, void* Vc,
+                             const int32_t* table, const int32_t* len, int32_t* len_out, float* acc_score,
+                             int32_t* pos_cache, const lvlm_dims* d, int32_t* dev_status, void* stream);
+
+/*
+ * Appends rows of a contiguous cache to another cache: the accepted path of a tree of drafts, or (index = NULL,
+ * d->count_heads = 1, count = the lengths) a whole ragged cache that moves into pages.
+ *   K[b,g,len[b,g] + i] = Kd[b,g,index[b,i]],  V the same,  i < count;   len_out[b,g] = len[b,g] + count
+ *   index      optional [B][T] int32, any rows of Kd in any order (one outside [0, draft_cap) sets LVLM_DEV_BOUNDS and its row is
+ *              skipped); NULL = rows 0, 1, 2, ...
+ *   count      [B] int32, or with d->count_heads [B][Hkv]; NULL = T
+ *   pos        optional [B][draft_cap] int32: positions of the rows of Kd, gathered into pos_cache (both or neither)
+ *   len, len_out, acc_score, pos_cache: as in lvlm_rope_append.  Kd and Vd may not overlap Kc and Vc.
+ * Reads d: B,Hkv,D,T,draft_cap,draft_stride_*,count_heads, and the cache's fields.
+ * Errors: INVALID_ARG (also T > draft_cap without an index, Kd == Kc, Vd == Vc, pos without pos_cache or the reverse),
+ * UNSUPPORTED, ALIGNMENT.
+ */
+lvlm_status lvlm_commit_rows(const void* Kd, const void* Vd, const int32_t* index, const int32_t* count,
+                             const int32_t* pos, void* Kc, void* Vc, const int32_t* table, const int32_t* len,
+                             int32_t* len_out, float* acc_score, int32_t* pos_cache, const lvlm_dims* d,
+                             int32_t* dev_status, void* stream);
+
+/*
+ * Attention of the drafted tokens of every sequence over its cache and over one another.
+ *   visible(b,g,t) = { cache rows j < len[b,g] } and { drafts u < count[b] : t sees u }
+ *   out[b,t,h,:]   = softmax over visible of (q[b,t,h] . k * scale), applied to the values, g = h/(H/Hkv), t < count[b]
+ *   lse[b,h,t]     = natural log of the sum of the exponentials of the scaled logits
+ * A row that sees nothing gives out = 0 and lse = -inf.  With one draft a sequence this is decode attention over either kind
+ * of cache.
+ *   q        [B][T][H][D] bf16 (strides d->q_stride_*)     out  [B][T][H][D] bf16, packed
+ *   len      [B][Hkv] int32                                lse  optional [B][H][T] fp32
+ *   Kd, Vd   [B][Hkv][draft_cap][D] bf16, the drafts' keys (rotated) and values, or both NULL: only the cache is seen
+ *   mask     [B][T][(T+31)/32] uint32 ([T][(T+31)/32] with d->mask_shared): bit u % 32 of word u / 32 of row t set = t sees
+ *            draft u (its ancestors and, as a rule, itself); NULL = a chain, t sees the drafts u <= t
+ * Rows behind len and behind count may hold anything, NaN included; the rows in front of them are finite.
+ * d->N, optional: how many rows the caller expects a head to hold at most (0 = unknown): how the work is split over the GPU then
+ * goes by it instead of the capacity.  It changes no result beyond rounding.
+ * Workspace: the partial results where a head's keys are split; lvlm_workspace_bytes(LVLM_OP_TREE_ATTN, d).  Calls that may
+ * overlap on the GPU need workspaces of their own.
+ * Reads d: B,H,Hkv,D,N,T,draft_cap,mask_shared,q_stride_*,draft_stride_*, and the cache's fields.
+ * Errors: INVALID_ARG (NULL q/Kc/Vc/len/out, one of Kd/Vd, a mask without drafts, draft_cap < T, scale <= 0), UNSUPPORTED
+ * (D != 128, T > 256, H/Hkv > 64), ALIGNMENT, WORKSPACE.  Contents of out and lse are undefined when a kernel gave up on a
+ * wait and set LVLM_DEV_TIMEOUT.
+ */
+lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void* Vc, const int32_t* table, const int32_t* len,
+                           const void* Kd, const void* Vd, const uint32_t* mask, const int32_t* count,
+                           const lvlm_dims* d, float scale, void* out, float* lse,
+                           void* ws, size_t ws_bytes, int32_t* dev_status, void* stream);
 
 #ifdef __cplusplus
 }

@@ -19,11 +19,11 @@ _LIB_PATH = os.path.join(_PKG, "liblvlm.so")
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_WORKSPACE, ERR_CUDA = range(6)
 DEV_NONFINITE, DEV_TIMEOUT, DEV_BOUNDS = 1, 2, 4
 W_LINEAR_RANK, W_GEOMETRIC, W_UNIFORM, W_CUSTOM, W_NEAREST_KEPT = range(5)
-OP_SCORE_TOKENS, OP_SELECT_TOPK, OP_MERGE_COMPACT, OP_KV_COMPRESS, OP_DECODE_ATTN, OP_PREFILL_ATTN = range(6)
+OP_SCORE_TOKENS, OP_SELECT_TOPK, OP_MERGE_COMPACT, OP_KV_COMPRESS, OP_DECODE_ATTN, OP_PREFILL_ATTN, OP_TREE_ATTN = range(7)
 
 EXPORTS = ("lvlm_version", "lvlm_status_string", "lvlm_workspace_bytes", "lvlm_score_tokens",
            "lvlm_select_topk", "lvlm_merge_compact", "lvlm_kv_compress", "lvlm_decode_attn",
-           "lvlm_decode_attn_static", "lvlm_prefill_attn")
+           "lvlm_decode_attn_static", "lvlm_prefill_attn", "lvlm_rope_append", "lvlm_commit_rows", "lvlm_tree_attn")
 STATIC_SCRATCH_BYTES = 4 << 20
 
 
@@ -34,7 +34,12 @@ class Dims(ctypes.Structure):
                  "recent", "merge_mode", "cache_stable")] + \
                [(n, ctypes.c_int64) for n in
                 ("q_stride_b", "q_stride_n", "q_stride_h", "kv_stride_b", "kv_stride_h",
-                 "hid_stride_b", "out_stride_b", "head_stride")]
+                 "hid_stride_b", "out_stride_b", "head_stride")] + \
+               [(n, ctypes.c_int32) for n in
+                ("T", "page", "n_pages", "max_pages", "draft_cap", "rot", "interleaved", "n_pos", "axes", "sect0", "sect1",
+                 "count_heads", "mask_shared")] + \
+               [(n, ctypes.c_int64) for n in
+                ("new_stride_b", "new_stride_n", "new_stride_h", "page_stride", "draft_stride_b", "draft_stride_h")]
 
 
 class LvlmError(RuntimeError):
@@ -87,6 +92,12 @@ def lib() -> ctypes.CDLL:
         L.lvlm_decode_attn_static.argtypes = [vp, vp, vp, vp, vp, vp, vp, dp, f32, vp, vp, vp]
         L.lvlm_prefill_attn.restype = ctypes.c_int
         L.lvlm_prefill_attn.argtypes = [vp, vp, vp, dp, f32, vp, vp, vp, vp, vp, sz, vp, vp]
+        L.lvlm_rope_append.restype = ctypes.c_int
+        L.lvlm_rope_append.argtypes = [vp] * 14 + [dp, vp, vp]
+        L.lvlm_commit_rows.restype = ctypes.c_int
+        L.lvlm_commit_rows.argtypes = [vp] * 12 + [dp, vp, vp]
+        L.lvlm_tree_attn.restype = ctypes.c_int
+        L.lvlm_tree_attn.argtypes = [vp] * 9 + [dp, f32, vp, vp, vp, sz, vp, vp]
         _lib = L
     return _lib
 
@@ -328,3 +339,214 @@ def decode_attn_static(q, Kc, Vc, length, *, k_new=None, v_new=None, acc_score=N
                                          scale, _ptr(out), _ptr(dev_status),
                                          _stream(stream)), "lvlm_decode_attn_static")
     return out
+
+
+# ---- several new tokens at a time, and paged caches -------------------------------------------
+# A cache is contiguous, [B,Hkv,cap,D] (table None), or paged, [n_pages,page,D] with table [B,Hkv,max_pages] int32.
+_BF16, _I32, _F32 = torch.bfloat16, torch.int32, torch.float32
+
+
+def _arg(t: Optional[torch.Tensor], name: str, dtype, shape, device, last_packed_only=False) -> Optional[int]:
+    """Pointer of an optional argument after the checks that the C call cannot make."""
+    if t is None:
+        return None
+    if not t.is_cuda:
+        raise TypeError("lvlm works on CUDA tensors only; there is no CPU path")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} has to be {dtype}, not {t.dtype}")
+    if t.device != device:
+        raise ValueError(f"{name} is on {t.device}, the other tensors on {device}")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} has to have the shape {tuple(shape)}, not {tuple(t.shape)}")
+    if t.stride(-1) != 1 and t.shape[-1] > 1 if last_packed_only else not t.is_contiguous():
+        raise ValueError(f"{name} has to be " + ("contiguous in its last dimension" if last_packed_only else "contiguous"))
+    return t.data_ptr()
+
+
+def _strides(t: torch.Tensor, name: str, n: int):
+    """The first n strides for the C call: 0 (packed) for a dimension of one element, whose stride means nothing."""
+    st = tuple(x if size > 1 else 0 for x, size in zip(t.stride()[:n], t.shape))
+    if any(x == 0 and size > 1 for x, size in zip(st, t.shape)):
+        raise ValueError(f"{name} repeats its elements along a dimension (an expanded view)")
+    return st
+
+
+def _device(t: torch.Tensor) -> torch.device:
+    if t.is_cuda and t.device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return t.device
+
+
+def _cache(d: Dims, Kc, Vc, table, B, Hkv, device):
+    """Fills the cache's fields of ``d``; returns the three pointers."""
+    kp = _arg(Kc, "Kc", _BF16, None, device, True)
+    vp = _arg(Vc, "Vc", _BF16, Kc.shape, device, True)
+    if Vc.stride() != Kc.stride() or Kc.stride(-2) != Kc.shape[-1] and Kc.shape[-2] > 1:
+        raise ValueError("Kc and Vc have to have the same strides and packed rows")
+    if table is None:
+        if Kc.dim() != 4 or Kc.shape[0] != B or Kc.shape[1] != Hkv:
+            raise ValueError(f"a contiguous cache has the shape [{B}, {Hkv}, cap, D], not {tuple(Kc.shape)}")
+        d.cap, d.D = Kc.shape[2], Kc.shape[3]
+        d.kv_stride_b, d.kv_stride_h = _strides(Kc, "Kc", 2)
+        return kp, vp, None
+    if Kc.dim() != 3 or table.dim() != 3:
+        raise ValueError("a paged cache has the shape [n_pages, page, D], its table [B, Hkv, max_pages]")
+    d.n_pages, d.page, d.D = Kc.shape
+    (d.page_stride,), d.max_pages = _strides(Kc, "Kc", 1), table.shape[2]
+    return kp, vp, _arg(table, "table", _I32, (B, Hkv, d.max_pages), device)
+
+
+def rope_table(n_pos: int, rot: int = 128, base: float = 10000.0, device="cuda") -> torch.Tensor:
+    """cos_sin [n_pos, rot] fp32 for ``rope_append``: cosines of the rot/2 frequencies base^(-2i/rot), then their sines.
+    The angles are formed in 64 bits: in 32 an angle of position p is off by p 2^-24 radians."""
+    freq = torch.tensor(base, dtype=torch.float64) ** (torch.arange(0, rot, 2, dtype=torch.float64) / -rot)
+    angle = torch.arange(n_pos, dtype=torch.float64)[:, None] * freq
+    return torch.cat([angle.cos(), angle.sin()], 1).to(_F32).to(device)
+
+
+def tree_mask(parents: torch.Tensor) -> torch.Tensor:
+    """Mask words for ``tree_attn`` of trees given by their parents [..., T]: draft t (parent < t, negative = the last token of
+    the cache) sees itself and what it descends from.  Returns [..., T, ceil(T/32)] int32 on the device of ``parents``."""
+    T, lead = parents.shape[-1], parents.shape[:-1]
+    par = parents.reshape(-1, T).cpu().tolist()
+    W = (T + 31) // 32
+    words = []
+    for row in par:
+        seen = []
+        for t, p in enumerate(row):
+            if p >= t:
+                raise ValueError(f"the parent of draft {t} is {p}: parents come before their children")
+            seen.append((seen[p] if p >= 0 else 0) | 1 << t)
+        words += [[(x >> (32 * w)) & 0xFFFFFFFF for w in range(W)] for x in seen]
+    m = torch.tensor(words, dtype=torch.int64).reshape(*lead, T, W)
+    return torch.where(m >= 1 << 31, m - (1 << 32), m).to(torch.int32).to(parents.device)
+
+
+def rope_append(k_new, v_new, pos, cos_sin, Kc, Vc, length=None, *, q=None, q_out=None, table=None, count=None, len_out=None,
+                sections=None, interleaved=False, acc_score=None, pos_cache=None, dev_status=None, stream=None):
+    """lvlm_rope_append.  k_new, v_new [B,T,Hkv,D] and q [B,T,H,D] (views with strides are fine) are rotated by
+    cos_sin[pos] and k_new, v_new are appended behind ``length`` [B,Hkv], which grows by ``count`` [B] (None = T): in place, or
+    into ``len_out``.  length None: the rows start at 0 (a draft cache), and no length is written unless len_out is given.
+    pos is [B,T], or [3,B,T] with ``sections`` (the frequencies that follow each axis); cos_sin None: nothing is rotated.
+    Returns q_out [B,T,H,D] (``q_out=q`` rotates in place) or None without q."""
+    dev = _device(k_new)
+    B, T, Hkv, D = k_new.shape
+    d = Dims(B=B, Hkv=Hkv, T=T, interleaved=int(interleaved))
+    kp, vp, tp = _cache(d, Kc, Vc, table, B, Hkv, dev)
+    if d.D != D:
+        raise ValueError(f"Kc has rows of {d.D} channels, k_new of {D}")
+    knp = _arg(k_new, "k_new", _BF16, None, dev, True)
+    vnp = _arg(v_new, "v_new", _BF16, k_new.shape, dev, True)
+    if v_new.stride() != k_new.stride():
+        raise ValueError("k_new and v_new have to have the same strides")
+    d.new_stride_b, d.new_stride_n, d.new_stride_h = _strides(k_new, "k_new", 3)
+    qp = qop = None
+    if q is not None:
+        H = q.shape[2]
+        qp = _arg(q, "q", _BF16, (B, T, H, D), dev, True)
+        d.H = H
+        d.q_stride_b, d.q_stride_n, d.q_stride_h = _strides(q, "q", 3)
+        if q_out is None:
+            q_out = torch.empty(B, T, H, D, dtype=_BF16, device=dev)
+        qop = q.data_ptr() if q_out is q else _arg(q_out, "q_out", _BF16, q.shape, dev)
+        if qop == qp and q_out.stride() != q.stride():
+            raise ValueError("q_out starts where q does but is laid out differently")
+    if cos_sin is not None:
+        d.n_pos, d.rot = cos_sin.shape
+    if sections is not None:
+        d.axes, d.sect0, d.sect1 = 3, sections[0], sections[1]
+        if len(sections) != 3 or sum(sections) != d.rot // 2:
+            raise ValueError(f"sections {tuple(sections)} do not share out {d.rot // 2} frequencies")
+    if len_out is None:
+        len_out = length
+    hs = (B, Hkv)
+    side = (B, Hkv, d.cap or d.page * d.max_pages)
+    _check(lib().lvlm_rope_append(
+        qp, knp, vnp, _arg(pos, "pos", _I32, (3, B, T) if sections is not None else (B, T), dev), _arg(cos_sin, "cos_sin", _F32, None, dev),
+        _arg(count, "count", _I32, (B,), dev), qop, kp, vp, tp, _arg(length, "length", _I32, hs, dev), _arg(len_out, "len_out", _I32, hs, dev),
+        _arg(acc_score, "acc_score", _F32, side, dev), _arg(pos_cache, "pos_cache", _I32, side, dev), ctypes.byref(d),
+        _arg(dev_status, "dev_status", _I32, None, dev), _stream(stream)), "lvlm_rope_append")
+    return q_out if q is not None else None
+
+
+def commit_rows(Kd, Vd, Kc, Vc, length, count=None, *, index=None, table=None, len_out=None, pos=None, acc_score=None,
+                pos_cache=None, dev_status=None, stream=None):
+    """lvlm_commit_rows.  Rows index[b,i] of Kd, Vd [B,Hkv,draft_cap,D] are appended to a cache behind ``length`` [B,Hkv], which
+    grows by ``count``: in place, or into ``len_out``.  count [B] (None = all) or, to move a ragged cache, [B,Hkv];
+    index [B,T] int32, None = the first rows."""
+    dev = _device(Kd)
+    B, Hkv, rows, D = Kd.shape
+    T = rows if index is None else index.shape[-1]
+    d = Dims(B=B, Hkv=Hkv, T=T, draft_cap=rows)
+    kp, vp, tp = _cache(d, Kc, Vc, table, B, Hkv, dev)
+    if d.D != D:
+        raise ValueError(f"Kc has rows of {d.D} channels, Kd of {D}")
+    kdp = _arg(Kd, "Kd", _BF16, None, dev, True)
+    vdp = _arg(Vd, "Vd", _BF16, Kd.shape, dev, True)
+    if Vd.stride() != Kd.stride() or Kd.stride(2) != D and rows > 1:
+        raise ValueError("Kd and Vd have to have the same strides and packed rows")
+    d.draft_stride_b, d.draft_stride_h = _strides(Kd, "Kd", 2)
+    hs = (B, Hkv)
+    d.count_heads = int(count is not None and count.dim() == 2)
+    side = (B, Hkv, d.cap or d.page * d.max_pages)
+    if len_out is None:
+        len_out = length
+    _check(lib().lvlm_commit_rows(
+        kdp, vdp, _arg(index, "index", _I32, (B, T), dev), _arg(count, "count", _I32, hs if d.count_heads else (B,), dev),
+        _arg(pos, "pos", _I32, (B, rows), dev), kp, vp, tp, _arg(length, "length", _I32, hs, dev), _arg(len_out, "len_out", _I32, hs, dev),
+        _arg(acc_score, "acc_score", _F32, side, dev), _arg(pos_cache, "pos_cache", _I32, side, dev), ctypes.byref(d),
+        _arg(dev_status, "dev_status", _I32, None, dev), _stream(stream)), "lvlm_commit_rows")
+
+
+def tree_dims(q, Kc, table=None, Kd=None, *, max_len=None) -> Dims:
+    """Sizes for ``alloc_workspace(OP_TREE_ATTN, ...)``."""
+    B, T, H, D = q.shape
+    d = Dims(B=B, H=H, T=T, D=D, N=max_len or 0)
+    if table is None:
+        d.Hkv, d.cap = Kc.shape[1], Kc.shape[2]
+    else:
+        d.Hkv, d.n_pages, d.page, d.max_pages = table.shape[1], Kc.shape[0], Kc.shape[1], table.shape[2]
+    if Kd is not None:
+        d.draft_cap = Kd.shape[2]
+    return d
+
+
+def tree_attn(q, Kc, Vc, length, *, Kd=None, Vd=None, mask=None, count=None, table=None, scale=None, out=None, lse=None,
+              want_lse=False, max_len=None, ws=None, dev_status=None, stream=None):
+    """lvlm_tree_attn.  q [B,T,H,D] (a view with strides is fine) attends to ``length`` [B,Hkv] rows of a cache and to the
+    drafts Kd, Vd [B,Hkv,>=T,D] that ``mask`` lets it see ([B,T,W] or [T,W] int32 words from ``tree_mask``; None = a chain).  count
+    [B]: drafts of each sequence (None = T).  max_len: rows a head is expected to hold at most, where the caller knows (it decides
+    how the work is split, not the result).  Returns (out [B,T,H,D], lse [B,H,T] or None); rows behind count are left as they were."""
+    dev = _device(q)
+    B, T, H, D = q.shape
+    d = tree_dims(q, Kc, table, Kd, max_len=max_len)
+    Hkv = d.Hkv
+    qp = _arg(q, "q", _BF16, None, dev, True)
+    d.q_stride_b, d.q_stride_n, d.q_stride_h = _strides(q, "q", 3)
+    kp, vp, tp = _cache(d, Kc, Vc, table, B, Hkv, dev)
+    if d.D != D:
+        raise ValueError(f"Kc has rows of {d.D} channels, q of {D}")
+    kdp = vdp = None
+    if Kd is not None:
+        kdp = _arg(Kd, "Kd", _BF16, (B, Hkv, Kd.shape[2], D), dev, True)
+        vdp = _arg(Vd, "Vd", _BF16, Kd.shape, dev, True)
+        if Vd is not None and Vd.stride() != Kd.stride() or Kd.stride(2) != D and Kd.shape[2] > 1:
+            raise ValueError("Kd and Vd have to have the same strides and packed rows")
+        d.draft_stride_b, d.draft_stride_h = _strides(Kd, "Kd", 2)
+    mp = None
+    if mask is not None:
+        W = (T + 31) // 32
+        d.mask_shared = int(mask.dim() == 2)
+        mp = _arg(mask, "mask", _I32, (T, W) if d.mask_shared else (B, T, W), dev)
+    if scale is None:
+        scale = 1.0 / math.sqrt(D)
+    if out is None:
+        out = torch.empty(B, T, H, D, dtype=_BF16, device=dev)
+    if lse is None and want_lse:
+        lse = torch.empty(B, H, T, dtype=_F32, device=dev)
+    ws, wsp, wsn = _ws(ws, OP_TREE_ATTN, d, dev)
+    _check(lib().lvlm_tree_attn(qp, kp, vp, tp, _arg(length, "length", _I32, (B, Hkv), dev), kdp, vdp, mp,
+                                _arg(count, "count", _I32, (B,), dev), ctypes.byref(d), scale, _arg(out, "out", _BF16, (B, T, H, D), dev),
+                                _arg(lse, "lse", _F32, (B, H, T), dev), wsp, wsn, _arg(dev_status, "dev_status", _I32, None, dev),
+                                _stream(stream)), "lvlm_tree_attn")
+    return out, lse

@@ -1,0 +1,441 @@
+"""Decoding several drafted tokens at a time on the GPU against the 64-bit oracle: append with rotation, tree attention, commit."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import draft_oracle as DO
+from paper_2509_00419_b200 import binding as L
+from tests.util import f64, i32
+
+pytestmark = pytest.mark.gpu
+BF = torch.bfloat16
+
+
+def bf(r, *shape):
+    return torch.from_numpy(r.normal(size=shape).astype(np.float32)).to(BF)
+
+
+def dev(x, dtype=np.int32):
+    return torch.from_numpy(np.ascontiguousarray(np.asarray(x, dtype))).cuda()
+
+
+def flag():
+    return torch.zeros(1, dtype=torch.int32, device="cuda")
+
+
+def paged(r, K, V, page, fill=float("nan"), spare=3):
+    """A logical cache [B][Hkv][cap][D] (cap a multiple of page) in shuffled pages: (Kp, Vp, table)."""
+    B, Hkv, cap, D = K.shape
+    mp = cap // page
+    n_pages = B * Hkv * mp + spare
+    table = r.permutation(n_pages)[:B * Hkv * mp].reshape(B, Hkv, mp)
+    kp, vp = (torch.full((n_pages, page, D), fill, dtype=BF) for _ in range(2))
+    at = torch.from_numpy(table).reshape(-1)
+    kp[at], vp[at] = K.reshape(-1, page, D), V.reshape(-1, page, D)
+    return kp.cuda(), vp.cuda(), dev(table)
+
+
+def logical(Kp, table):
+    """Back to [B][Hkv][cap][D]."""
+    t = table.long()
+    return Kp[t.reshape(-1)].reshape(*t.shape[:2], -1, Kp.shape[-1])
+
+
+def same(a, b):
+    """Bit for bit, NaN included."""
+    return torch.equal(a.cpu().contiguous().view(torch.int16), b.cpu().contiguous().view(torch.int16))
+
+
+# ---- append with rotation ----------------------------------------------------------------------------------------
+@pytest.mark.parametrize("B,H,Hkv,T,cap,page,rot,interleaved,sections,inplace", [
+    (1, 28, 4, 1, 37, 0, 128, False, None, True), (2, 8, 8, 1, 64, 16, 128, True, None, False), (3, 8, 2, 37, 100, 0, 64, False, None, False),
+    (2, 7, 1, 130, 256, 64, 128, False, (16, 24, 24), True), (2, 4, 4, 17, 64, 32, 32, True, (3, 7, 6), False),
+    (1, 2, 1, 5, 16, 16, 16, False, None, True), (2, 6, 2, 9, 128, 128, 0, False, None, True), (4, 48, 8, 3, 40, 0, 112, False, (0, 56, 0), False)])
+def test_rope_append(B, H, Hkv, T, cap, page, rot, interleaved, sections, inplace):
+    r = np.random.default_rng(B * 1000 + T * 10 + rot)
+    n_pos = 300
+    qkv = bf(r, B, T, H + 2 * Hkv, 128)
+    K, V = bf(r, B, Hkv, cap, 128), bf(r, B, Hkv, cap, 128)
+    ln = r.integers(0, cap - T + 1, size=(B, Hkv))
+    ln.reshape(-1)[0] = cap - T                                       # filled to the last row
+    count = r.integers(0, T + 1, size=B)
+    count[0] = T
+    pos = r.integers(0, n_pos, size=(3, B, T) if sections else (B, T))
+    table_cs = L.rope_table(n_pos, rot, 1000.0, device="cpu") if rot else None
+    cs = np.zeros((1, 0), np.float32) if rot == 0 else table_cs.numpy()
+    x = f64(qkv)
+    turn = (lambda v: v) if rot == 0 else (lambda v: DO.rotate(v, pos, cs, interleaved, sections))
+    want_q, k_rot = turn(x[:, :, :H]), turn(x[:, :, H:H + Hkv])
+    want_K, want_V, want_len = DO.append(f64(K), f64(V), ln, k_rot, x[:, :, H + Hkv:], count)
+
+    d = qkv.cuda()
+    q, kn, vn = d[:, :, :H], d[:, :, H:H + Hkv], d[:, :, H + Hkv:]
+    Kd, Vd, tab = paged(r, K, V, page) if page else (K.cuda(), V.cuda(), None)
+    ld, st = dev(ln), flag()
+    acc = torch.full((B, Hkv, cap), 5.0, device="cuda")
+    pc = torch.full((B, Hkv, cap), -7, dtype=torch.int32, device="cuda")
+    q_out = q if inplace else torch.full((B, T, H, 128), 3.0, dtype=BF, device="cuda")
+    len_out = None if inplace else torch.empty_like(ld)
+    got = L.rope_append(kn, vn, dev(pos), None if rot == 0 else table_cs.cuda(), Kd, Vd, ld, q=q, q_out=q_out, table=tab, count=dev(count),
+                        len_out=len_out, sections=sections, interleaved=interleaved, acc_score=acc, pos_cache=pc, dev_status=st)
+    torch.cuda.synchronize()
+    assert st.item() == 0 and got is q_out
+    assert np.array_equal(i32(ld if inplace else len_out), want_len) and (inplace or np.array_equal(i32(ld), ln))
+    # a rounding to bf16 (2^-8 of the value), two products and a sum in fp32 (2^-24 of a and b each, a and b below 2^3)
+    close = lambda a, b: np.abs(a - b) <= 2.0 ** -8 * np.abs(b) + 2.0 ** -20
+    for b in range(B):
+        n = count[b]
+        assert close(f64(q_out)[b, :n], want_q[b, :n]).all()
+        assert same(q_out[b, n:], d[b, n:, :H] if inplace else torch.full_like(q_out[b, n:], 3.0))
+    Kl, Vl = (Kd, Vd) if not page else (logical(Kd, tab), logical(Vd, tab))
+    assert close(f64(Kl), want_K).all() and np.array_equal(f64(Vl), want_V)
+    p0 = pos[0] if sections else pos
+    for b in range(B):
+        for g in range(Hkv):
+            lo, hi = ln[b, g], ln[b, g] + count[b]
+            assert same(Kl[b, g, :lo], K[b, g, :lo]) and same(Kl[b, g, hi:], K[b, g, hi:])
+            assert (acc[b, g, lo:hi] == 0).all() and (acc[b, g, :lo] == 5).all() and (acc[b, g, hi:] == 5).all()
+            assert np.array_equal(i32(pc[b, g, lo:hi]), p0[b, :count[b]]) and (pc[b, g, :lo] == -7).all() and (pc[b, g, hi:] == -7).all()
+    if not inplace:
+        assert same(d[:, :, :H], qkv[:, :, :H])
+    if page:
+        other = sorted(set(range(Kd.shape[0])) - set(i32(tab).reshape(-1).tolist()))
+        assert torch.isnan(Kd[other]).all() and torch.isnan(Vd[other]).all()
+
+
+def test_rope_append_into_a_draft_cache_without_queries():
+    r = np.random.default_rng(7)
+    kn, vn = bf(r, 2, 6, 3, 128), bf(r, 2, 6, 3, 128)
+    Kd, Vd = (torch.full((2, 3, 9, 128), 2.0, dtype=BF, device="cuda") for _ in range(2))
+    st = flag()
+    assert L.rope_append(kn.cuda(), vn.cuda(), None, None, Kd, Vd, dev_status=st) is None
+    assert st.item() == 0 and same(Kd[:, :, :6], kn.transpose(1, 2)) and same(Vd[:, :, :6], vn.transpose(1, 2))
+    assert (Kd[:, :, 6:] == 2).all() and (Vd[:, :, 6:] == 2).all()
+
+
+def test_rope_append_flags():
+    """Heads and tokens that cannot be served are skipped and flagged; the others are served."""
+    r = np.random.default_rng(8)
+    B, Hkv, T, page = 5, 2, 4, 16
+    K, V = bf(r, B, Hkv, 32, 128), bf(r, B, Hkv, 32, 128)
+    kn, vn, q = bf(r, B, T, Hkv, 128), bf(r, B, T, Hkv, 128), bf(r, B, T, 4, 128)
+    cs = L.rope_table(50, 128, 100.0)
+    good_len = np.array([[0, 5], [28, 3], [12, 20], [7, 7], [14, 1]])
+    pos = np.arange(B * T).reshape(B, T)
+
+    def go(ln=good_len, count=np.full(B, T), p=pos, broken=None):
+        Kp, Vp, tab = paged(np.random.default_rng(9), K, V, page)
+        if broken is not None:
+            tab[broken[0], broken[1], broken[2]] = broken[3]
+        ld, st, qo = dev(ln), flag(), torch.zeros_like(q).cuda()
+        L.rope_append(kn.cuda(), vn.cuda(), dev(p), cs, Kp, Vp, ld, q=q.cuda(), q_out=qo, table=tab, count=dev(count), dev_status=st)
+        return st.item(), i32(ld), Kp, Vp, tab, qo
+
+    s0, l0, K0, V0, t0, q0 = go()
+    assert s0 == 0 and np.array_equal(l0, good_len + T)
+    for bad in (-1, 33, 29, 1 << 30, -(1 << 31)):                    # 29: the rows do not fit
+        ln = good_len.copy()
+        ln[1, 1] = bad
+        s, l, K1, V1, t, q1 = go(ln)
+        assert s == L.DEV_BOUNDS and l[1, 1] == bad and same(q1, q0)
+        keep = np.ones((B, Hkv), bool)
+        keep[1, 1] = False
+        assert np.array_equal(l[keep], l0[keep])
+        lg, lg0 = logical(K1, t), logical(K0, t0)
+        assert same(lg[1, 1], K[1, 1]) and same(lg[torch.from_numpy(keep)], lg0[torch.from_numpy(keep)])
+    for bad in (-1, 5):
+        c = np.full(B, T)
+        c[2] = bad
+        s, l, K1, _, t, q1 = go(count=c)
+        assert s == L.DEV_BOUNDS and np.array_equal(l[2], good_len[2]) and same(logical(K1, t)[2], K[2]) and (q1[2] == 0).all()
+        assert same(q1[3], q0[3]) and np.array_equal(l[3], l0[3])
+    for bad in (-1, 23, 1 << 30):                                    # 20 pages and 3 spare ones: 23 is the first that is none
+        s, l, K1, _, t, q1 = go(broken=(4, 0, 0, bad))               # rows 14, 15 of this head are lost, 16 and 17 arrive
+        assert s == L.DEV_BOUNDS and l[4, 0] == 18 and same(q1, q0)
+        assert same(K1[t0[4, 0, 1].item(), :2], K0[t0[4, 0, 1].item(), :2]) and same(K1[t0[4, 0, 0].item()], K[4, 0, :16])
+    p = pos.copy()
+    p[3, 2] = 50
+    s, _, K1, _, t, q1 = go(p=p)
+    assert s == L.DEV_BOUNDS and same(q1[3, 2], q[3, 2]) and same(logical(K1, t)[3, 0, 9], kn[3, 2, 0]) and same(q1[3, 1], q0[3, 1])
+
+
+# ---- commit ----------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("B,Hkv,rows,T,cap,page,inplace", [
+    (1, 1, 1, 1, 3, 0, True), (3, 4, 7, 7, 48, 16, True), (2, 2, 9, 30, 96, 32, False), (2, 3, 65, 65, 192, 64, True), (2, 1, 300, 300, 400, 0, False),
+    (1, 2, 130, 64, 128, 128, True)])
+def test_commit_path(B, Hkv, rows, T, cap, page, inplace):
+    r = np.random.default_rng(rows + T)
+    K, V, Kd, Vd = bf(r, B, Hkv, cap, 128), bf(r, B, Hkv, cap, 128), bf(r, B, Hkv, rows, 128), bf(r, B, Hkv, rows, 128)
+    ln = r.integers(0, cap - T + 1, size=(B, Hkv))
+    ln.reshape(-1)[-1] = cap - T
+    count = r.integers(0, T + 1, size=B)
+    count[-1] = T
+    index = r.integers(0, rows, size=(B, T))                          # any order, the same row twice
+    pos = r.integers(0, 9999, size=(B, rows))
+    want = DO.commit(f64(K), f64(V), ln, f64(Kd), f64(Vd), index, count)
+    Kc, Vc, tab = paged(r, K, V, page) if page else (K.cuda(), V.cuda(), None)
+    ld, st = dev(ln), flag()
+    lo = None if inplace else torch.empty_like(ld)
+    acc = torch.full((B, Hkv, cap), 5.0, device="cuda")
+    pc = torch.full((B, Hkv, cap), -7, dtype=torch.int32, device="cuda")
+    bad = index.copy()
+    for b in range(B):
+        bad[b, count[b]:] = 1 << 30                                   # entries behind count are not read
+    L.commit_rows(Kd.cuda(), Vd.cuda(), Kc, Vc, ld, dev(count), index=dev(bad), table=tab, len_out=lo, pos=dev(pos), acc_score=acc,
+                  pos_cache=pc, dev_status=st)
+    torch.cuda.synchronize()
+    assert st.item() == 0
+    Kl, Vl = (Kc, Vc) if not page else (logical(Kc, tab), logical(Vc, tab))
+    assert np.array_equal(f64(Kl), want[0]) and np.array_equal(f64(Vl), want[1]) and np.array_equal(i32(ld if inplace else lo), want[2])
+    for b in range(B):
+        for g in range(Hkv):
+            a, z = ln[b, g], ln[b, g] + count[b]
+            assert (acc[b, g, a:z] == 0).all() and (acc[b, g, :a] == 5).all() and (acc[b, g, z:] == 5).all()
+            assert np.array_equal(i32(pc[b, g, a:z]), pos[b, index[b, :count[b]]]) and (pc[b, g, z:] == -7).all()
+
+
+@pytest.mark.parametrize("rows,page", [(40, 16), (200, 64), (200, 0), (64, 32)])
+def test_commit_moves_a_ragged_cache(rows, page):
+    r = np.random.default_rng(rows)
+    B, Hkv, cap = 3, 2, 256
+    Kd, Vd = bf(r, B, Hkv, rows, 128), bf(r, B, Hkv, rows, 128)
+    ln = r.integers(0, rows + 1, size=(B, Hkv))
+    ln.reshape(-1)[:3] = [0, rows, 1]
+    K, V = bf(r, B, Hkv, cap, 128), bf(r, B, Hkv, cap, 128)
+    want = DO.commit(f64(K), f64(V), np.zeros((B, Hkv), int), f64(Kd), f64(Vd), None, ln)
+    Kc, Vc, tab = paged(r, K, V, page) if page else (K.cuda(), V.cuda(), None)
+    ld, st = dev(np.zeros((B, Hkv))), flag()
+    # the source is a part of a larger cache, as compression leaves it
+    wide = torch.full((B, Hkv, rows + 9, 128), float("nan"), dtype=BF, device="cuda")
+    wide2 = wide.clone()
+    wide[:, :, :rows], wide2[:, :, :rows] = Kd.cuda(), Vd.cuda()
+    L.commit_rows(wide[:, :, :rows], wide2[:, :, :rows], Kc, Vc, ld, dev(ln), table=tab, dev_status=st)
+    torch.cuda.synchronize()
+    Kl, Vl = (Kc, Vc) if not page else (logical(Kc, tab), logical(Vc, tab))
+    assert st.item() == 0 and np.array_equal(i32(ld), ln)
+    assert np.array_equal(f64(Kl), want[0]) and np.array_equal(f64(Vl), want[1])
+
+
+def test_commit_flags():
+    r = np.random.default_rng(11)
+    B, Hkv, T = 4, 2, 5
+    Kd, Vd, K, V = bf(r, B, Hkv, T, 128), bf(r, B, Hkv, T, 128), bf(r, B, Hkv, 32, 128), bf(r, B, Hkv, 32, 128)
+
+    def go(ln=np.full((B, Hkv), 3), count=np.full(B, T), index=np.arange(T)[None].repeat(B, 0)):
+        Kc, Vc, ld, st = K.cuda(), V.cuda(), dev(ln), flag()
+        L.commit_rows(Kd.cuda(), Vd.cuda(), Kc, Vc, ld, dev(count), index=dev(index), dev_status=st)
+        return st.item(), i32(ld), Kc, Vc
+
+    s0, l0, K0, V0 = go()
+    assert s0 == 0 and (l0 == 8).all()
+    for bad in (-1, 28, 33):
+        ln = np.full((B, Hkv), 3)
+        ln[2, 1] = bad
+        s, l, Kc, _ = go(ln=ln)
+        assert s == L.DEV_BOUNDS and l[2, 1] == bad and same(Kc[2, 1], K[2, 1]) and same(Kc[2, 0], K0[2, 0]) and (l[:2] == 8).all()
+    for bad in (-3, 6):
+        s, l, Kc, _ = go(count=np.array([T, bad, T, T]))
+        assert s == L.DEV_BOUNDS and (l[1] == 3).all() and same(Kc[1], K[1]) and same(Kc[2], K0[2])
+    for bad in (-1, T, 1 << 30):
+        index = np.arange(T)[None].repeat(B, 0)
+        index[0, 2] = bad
+        s, l, Kc, _ = go(index=index)
+        assert s == L.DEV_BOUNDS and (l == 8).all() and same(Kc[0, :, 5], K[0, :, 5]) and same(Kc[0, :, 6], K0[0, :, 6]) and same(Kc[1], K0[1])
+
+
+# ---- tree attention ----------------------------------------------------------------------------------------------
+def tree_bound(q, K, V, n_keys, scale):
+    """What a result may be off beside its rounding, from the arithmetic.  A logit: 128 exact products added in fp32, each addition
+    off by at most 2^-23 of the running sum of magnitudes (the tensor core truncates), scaled once.  A probability: that, the
+    exponential (2^-22), the remainder of its two bf16 parts (2^-17).  The sums over the keys: 2^-23 an addition."""
+    mags = np.sqrt((q ** 2).sum(-1).max()) * np.sqrt((K ** 2).sum(-1).max()) * scale
+    logit = mags * 128 * 2.0 ** -23
+    prob = logit + 2.0 ** -22 + 2.0 ** -17 + n_keys * 2.0 ** -23
+    return 2 * prob * np.abs(V).max(), logit + (n_keys + 8) * 2.0 ** -23
+
+
+def random_tree(r, T, kind):
+    if kind == "chain":
+        return np.tril(np.ones((T, T), bool)), None
+    if kind == "any":                                                 # no tree at all; some rows see no draft
+        see = r.random((T, T)) < 0.4
+        see[r.integers(0, T)] = False
+        return see, None
+    par = [int(r.integers(-1, t)) if t else -1 for t in range(T)]
+    see = np.zeros((T, T), bool)
+    for t, p in enumerate(par):
+        see[t] = see[p] if p >= 0 else False
+        see[t, t] = True
+    return see, par
+
+
+def words_of(see):
+    T = see.shape[-1]
+    W = (T + 31) // 32
+    pad = np.zeros((*see.shape[:-1], W * 32), bool)
+    pad[..., :T] = see
+    return dev(np.packbits(pad, axis=-1, bitorder="little").view(np.uint32).reshape(*see.shape[:-1], W).astype(np.int64).astype(np.uint32).view(np.int32))
+
+
+def run_tree(B, H, Hkv, T, lens, count, page, kind, seed, max_len=None, shared=False, fill=float("nan"), drafts=True, spread=1.0, cap=None):
+    r = np.random.default_rng(seed)
+    lens = np.asarray(lens).reshape(B, Hkv)
+    unit = page or 1
+    cap = (cap or max(int(lens.max()), 1)) + (0 if page else 3)
+    cap = (cap + unit - 1) // unit * unit
+    q = (bf(r, B, T, H + 1, 128).float() * spread).to(BF)             # a view with strides
+    K, V = bf(r, B, Hkv, cap, 128), bf(r, B, Hkv, cap, 128)
+    Kd, Vd = bf(r, B, Hkv, T + 2, 128), bf(r, B, Hkv, T + 2, 128)
+    see = np.stack([random_tree(r, T, kind)[0] for _ in range(B)])
+    if shared:
+        see[:] = see[0]
+    count = np.asarray(count)
+    qf, scale = f64(q)[:, :, :H], 1 / np.sqrt(128)
+    out, lse = DO.tree_attn(qf, f64(K), f64(V), lens, f64(Kd) if drafts else None, f64(Vd), see, count)
+    o_tol, l_tol = tree_bound(qf, np.concatenate([f64(K), f64(Kd)], 2), np.concatenate([f64(V), f64(Vd)], 2), cap + T, scale)
+    for b in range(B):                                               # what lies behind holds anything
+        Kd[b, :, count[b]:], Vd[b, :, count[b]:] = fill, fill
+        for g in range(Hkv):
+            K[b, g, lens[b, g]:], V[b, g, lens[b, g]:] = fill, fill
+    Kc, Vc, tab = paged(r, K, V, page, fill) if page else (K.cuda(), V.cuda(), None)
+    mask = None if kind == "chain" or not drafts else words_of(see[0] if shared else see)
+    o = torch.full((B, T, H, 128), 9.0, dtype=BF, device="cuda")
+    ls = torch.full((B, H, T), 9.0, device="cuda")
+    st = flag()
+    args = dict(Kd=Kd.cuda()[:, :, :T + 2] if drafts else None, Vd=Vd.cuda() if drafts else None, mask=mask, count=dev(count), table=tab,
+                max_len=max_len, dev_status=st)
+    got, gl = L.tree_attn(q.cuda()[:, :, :H], Kc, Vc, dev(lens), out=o, lse=ls, **args)
+    torch.cuda.synchronize()
+    assert st.item() == 0 and got is o and gl is ls
+    for b in range(B):
+        n = count[b]
+        a, w = f64(o)[b, :n], out[b, :n]
+        err = np.abs(a - w) - 2.0 ** -8 * np.abs(w)
+        assert np.isfinite(a).all() and err.size == 0 or err.max() <= o_tol, (b, err.max(), o_tol)
+        assert (o[b, n:] == 9).all() and (ls[b, :, n:] == 9).all()
+        x, y = f64(ls)[b, :, :n], lse[b, :, :n]
+        assert np.array_equal(np.isinf(x), np.isinf(y)) and (x[np.isinf(x)] < 0).all()
+        fin = np.isfinite(y)
+        assert (np.abs(x[fin] - y[fin]) <= l_tol + 2.0 ** -22 * np.abs(y[fin])).all()
+        assert (a[np.isinf(np.transpose(y))] == 0).all()              # a row that sees nothing
+    again, _ = L.tree_attn(q.cuda()[:, :, :H], Kc, Vc, dev(lens), out=o.clone(), **args)
+    assert same(again, o)                                            # the same bits from run to run
+    return o
+
+
+@pytest.mark.parametrize("page", [0, 16, 32, 64, 128, 256])
+@pytest.mark.parametrize("B,H,Hkv,T,lens,count,kind", [
+    (1, 1, 1, 1, [0], [1], "chain"), (1, 1, 1, 1, [1], [1], "chain"), (1, 28, 4, 1, [216, 1, 0, 64], [1], "chain"),
+    (2, 8, 2, 5, [63, 64, 65, 0], [5, 3], "tree"), (3, 4, 4, 9, [0, 15, 16, 17, 31, 32, 33, 127, 128, 129, 0, 1], [9, 0, 4], "any"),
+    (1, 32, 8, 33, [130, 128, 100, 40, 257, 5, 64, 200], [33], "tree"), (2, 7, 1, 61, [300, 20], [61, 32], "tree"),
+    (1, 12, 2, 64, [500, 0], [64], "any"), (1, 5, 1, 65, [90], [65], "chain"), (2, 6, 1, 1, [70, 2], [1, 0], "any")])
+def test_tree_attn(page, B, H, Hkv, T, lens, count, kind):
+    run_tree(B, H, Hkv, T, lens, count, page, kind, seed=T + H)
+
+
+@pytest.mark.parametrize("B,H,Hkv,T,lens,count,kind,page", [
+    (1, 2, 1, 256, [40], [256], "tree", 0), (1, 1, 1, 129, [0], [129], "any", 0), (1, 3, 1, 200, [129], [160], "any", 64),
+    (1, 64, 1, 5, [150], [5], "tree", 16), (1, 40, 1, 3, [7], [3], "chain", 0), (1, 8, 1, 17, [1000], [17], "tree", 32)])
+def test_tree_attn_wide(B, H, Hkv, T, lens, count, kind, page):
+    run_tree(B, H, Hkv, T, lens, count, page, kind, seed=T)
+
+
+@pytest.mark.parametrize("max_len", [None, 1, 100, 3001, 100000])
+@pytest.mark.parametrize("T,page", [(1, 0), (3, 64), (20, 16)])
+def test_tree_attn_split_however(max_len, T, page):
+    """However the keys of a head are split, and whatever length was expected."""
+    run_tree(1, 4, 2, T, [3001, 170], [T], page, "tree", seed=T, max_len=max_len)
+    run_tree(1, 4, 2, T, [40, 0], [T], page, "tree", seed=T, max_len=max_len, cap=3000)
+
+
+def test_tree_attn_shared_mask_large_logits_no_drafts():
+    run_tree(3, 8, 2, 12, [50, 9, 0, 100, 64, 128], [12, 5, 12], 16, "any", seed=1, shared=True)
+    run_tree(2, 8, 2, 12, [50, 9, 0, 100], [12, 5], 0, "any", seed=2, drafts=False)
+    run_tree(2, 8, 2, 12, [50, 9, 70, 100], [12, 5], 0, "any", seed=3, spread=30.0)
+    run_tree(2, 8, 2, 12, [50, 9, 70, 100], [12, 5], 64, "any", seed=3, fill=float("inf"))
+
+
+def test_tree_attn_flags():
+    """A bad length, count or page number: flagged, nothing outside is read, the other heads are as without it."""
+    r = np.random.default_rng(12)
+    B, H, Hkv, T, page = 2, 4, 2, 3, 16
+    K, V, Kd, Vd, q = bf(r, B, Hkv, 48, 128), bf(r, B, Hkv, 48, 128), bf(r, B, Hkv, T, 128), bf(r, B, Hkv, T, 128), bf(r, B, T, H, 128)
+    Kp, Vp, tab = paged(r, K, V, page, fill=0.0)
+
+    def go(ln=((40, 20), (33, 7)), count=(T, T), broken=None):
+        t = tab.clone()
+        if broken is not None:
+            t[0, 1, 0] = broken
+        st, o = flag(), torch.full((B, T, H, 128), 9.0, dtype=BF, device="cuda")
+        _, l = L.tree_attn(q.cuda(), Kp, Vp, dev(ln), Kd=Kd.cuda(), Vd=Vd.cuda(), table=t, count=dev(count), out=o, want_lse=True, dev_status=st)
+        return st.item(), o, l
+
+    s0, o0, l0 = go()
+    assert s0 == 0
+    for bad in (-1, 49, 1 << 30):
+        s, o, l = go(ln=((40, 20), (bad, 7)))
+        assert s == L.DEV_BOUNDS and (o[1, :, :2] == 0).all() and torch.isneginf(l[1, :2]).all()
+        assert same(o[0], o0[0]) and same(o[1, :, 2:], o0[1, :, 2:])
+    for bad in (-1, 4):
+        s, o, _ = go(count=(T, bad))
+        assert s == L.DEV_BOUNDS and (o[1] == 9).all() and same(o[0], o0[0])
+    zeroed = K.clone(), V.clone()
+    for x in zeroed:
+        x[0, 1, :16] = 0                                             # the page's rows are taken as zeros
+    see = np.tril(np.ones((T, T), bool))[None].repeat(B, 0)
+    want, _ = DO.tree_attn(f64(q), f64(zeroed[0]), f64(zeroed[1]), np.array([[40, 20], [33, 7]]), f64(Kd), f64(Vd), see, [T, T])
+    tol, _ = tree_bound(f64(q), f64(K), f64(V), 51, 1 / np.sqrt(128))
+    for bad in (-1, Kp.shape[0], 1 << 30, -(1 << 31)):
+        s, o, _ = go(broken=bad)
+        assert s == L.DEV_BOUNDS and same(o[1], o0[1]) and same(o[0, :, :2], o0[0, :, :2])
+        assert (np.abs(f64(o) - want) <= 2.0 ** -8 * np.abs(want) + tol).all()
+
+
+def test_far_pages():
+    """A pool of more than 2^31 elements: every operator reaches its last page."""
+    page, n_pages = 128, (1 << 31) // (128 * 128) + 40
+    r = np.random.default_rng(13)
+    Kp = torch.empty(n_pages, page, 128, dtype=BF, device="cuda")
+    Vp = torch.empty_like(Kp)
+    tab = dev([[[n_pages - 1, 3, n_pages - 7]]])
+    B, T, H = 1, 40, 2
+    kn, vn, q = bf(r, B, 300, 1, 128), bf(r, B, 300, 1, 128), bf(r, B, T, H, 128)
+    ln = dev([[0]])
+    L.rope_append(kn.cuda(), vn.cuda(), None, None, Kp, Vp, ln, table=tab)
+    assert same(Kp[n_pages - 1], kn[0, :128, 0]) and same(Vp[n_pages - 7, :44], vn[0, 256:, 0])
+    Kd, Vd = bf(r, B, 1, T, 128), bf(r, B, 1, T, 128)
+    L.commit_rows(Kd.cuda(), Vd.cuda(), Kp, Vp, ln, table=tab)
+    assert same(Kp[n_pages - 7, 44:84], Kd[0, 0]) and ln.item() == 340
+    K = torch.cat([kn[:, :, 0], Kd[:, 0]], 1)[:, None]
+    V = torch.cat([vn[:, :, 0], Vd[:, 0]], 1)[:, None]
+    o, _ = L.tree_attn(q.cuda(), Kp, Vp, ln, table=tab)
+    want, _ = DO.tree_attn(f64(q), f64(K), f64(V), np.array([[340]]), None, None, None, [T])
+    tol, _ = tree_bound(f64(q), f64(K), f64(V), 340, 1 / np.sqrt(128))
+    assert (np.abs(f64(o) - want) <= 2.0 ** -8 * np.abs(want) + tol).all()
+
+
+def test_binding_refuses_what_the_call_cannot_see():
+    z = torch.zeros(2, 2, 16, 128, dtype=BF, device="cuda")
+    i = torch.zeros(2, 2, dtype=torch.int32, device="cuda")
+    q = torch.zeros(2, 3, 4, 128, dtype=BF, device="cuda")
+    for bad in (dict(q=q.half()), dict(Kc=z.float()), dict(length=i.long()), dict(Kd=z.half(), Vd=z.half()), dict(out=q.float()),
+                dict(count=torch.zeros(2, device="cuda"))):
+        with pytest.raises(TypeError):
+            L.tree_attn(**{**dict(q=q, Kc=z, Vc=z, length=i), **bad})
+    for bad in (dict(length=i[:1]), dict(Vc=z[:, :, :8]), dict(Kc=z.transpose(2, 3), Vc=z.transpose(2, 3)), dict(q=q[:, :, :1].expand(2, 3, 4, 128)),
+                dict(table=i[None].repeat(2, 1, 1)), dict(Kd=z, Vd=z, mask=torch.zeros(2, 3, 2, dtype=torch.int32, device="cuda")),
+                dict(out=q[:, :2]), dict(lse=torch.zeros(2, 4, 4, device="cuda")), dict(q=q[..., ::2])):
+        with pytest.raises(ValueError):
+            L.tree_attn(**{**dict(q=q, Kc=z, Vc=z, length=i), **bad})
+    kn = q[:, :, :2]
+    pos = torch.zeros(2, 3, dtype=torch.int32, device="cuda")
+    cs = L.rope_table(10)
+    for bad in (dict(v_new=kn.contiguous()), dict(pos=pos.T), dict(sections=(16, 24, 24)), dict(q=q, q_out=q[:, :2]), dict(len_out=i.view(-1)),
+                dict(acc_score=torch.zeros(2, 2, 15, device="cuda"))):
+        with pytest.raises(ValueError):
+            L.rope_append(**{**dict(k_new=kn, v_new=kn, pos=pos, cos_sin=cs, Kc=z, Vc=z, length=i), **bad})
+    with pytest.raises(ValueError):
+        L.commit_rows(z, z, z.clone(), z.clone(), i, torch.zeros(3, dtype=torch.int32, device="cuda"))
+    with pytest.raises(L.LvlmError):
+        L.commit_rows(z, z, z, z.clone(), i)
+    assert (i == 0).all()
