@@ -41,7 +41,7 @@ inline lvlm_status cache_geom(const lvlm_dims* d, const int32_t* table, CacheGeo
 // Device: element offset of row `row` (0 <= row < cap) of head hd = b * Hkv + g, or -1: its page number is not one of the pool.
 __device__ __forceinline__ int64_t cache_row(const CacheGeom& c, const int32_t* table, int b, int g, int row) {
     if (!c.page) return (int64_t)b * c.sb + (int64_t)g * c.sh + (int64_t)row * kHeadDim;
-    const int id = __ldg(table + ((int64_t)b * c.Hkv + g) * c.max_pages + (row >> c.shift));
+    const int id = *(table + ((int64_t)b * c.Hkv + g) * c.max_pages + (row >> c.shift));
     return id < 0 || id >= c.n_pages ? -1 : (int64_t)id * c.sh + (int64_t)(row & (c.page - 1)) * kHeadDim;
 }
 

@@ -33,7 +33,7 @@ __device__ __forceinline__ void flag_bounds(int32_t* dev_status) {
 // The new rows of a sequence or head: n of them, 0 where the number given is none.
 __device__ __forceinline__ int checked_count(const int32_t* count, int64_t at, int T, int32_t* dev_status) {
     if (!count) return T;
-    const int n = __ldg(count + at);
+    const int n = *(count + at);
     if (n < 0 || n > T) { flag_bounds(dev_status); return 0; }
     return n;
 }
@@ -87,12 +87,12 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeArg
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int axis = a.axes == 3 ? (f0 + i >= a.sect0) + (f0 + i >= a.sect0 + a.sect1) : 0;
-            const int p = __ldg(a.pos + ((int64_t)axis * a.B + b) * a.T + t);
+            const int p = *(a.pos + ((int64_t)axis * a.B + b) * a.T + t);
             const bool ok = p >= 0 && p < a.n_pos;
             if (!ok) flag_bounds(a.dev_status);
             const float* row = a.cos_sin + (int64_t)(ok ? p : 0) * a.rot + f0 + i;
-            cs[i] = ok ? __ldg(row) : 1.f;
-            sn[i] = ok ? __ldg(row + a.rot / 2) : 0.f;
+            cs[i] = ok ? *row : 1.f;
+            sn[i] = ok ? *(row + a.rot / 2) : 0.f;
         }
     }
     for (int r = group; r < a.H + 2 * Hkv; r += kRopeGroups) {
@@ -174,7 +174,7 @@ __global__ void __launch_bounds__(kCommitThreads) commit_rows_kernel(const Commi
         const int i = i0 + u * kStep + threadIdx.x / 16;
         off[u] = -1;
         if (i >= n) continue;
-        const int j = a.index ? __ldg(a.index + (int64_t)b * a.T + i) : i;
+        const int j = a.index ? *(a.index + (int64_t)b * a.T + i) : i;
         if (j < 0 || j >= a.draft_cap) { flag_bounds(a.dev_status); continue; }
         off[u] = cache_row(a.c, a.table, b, g, ln + i);
         if (off[u] < 0) { flag_bounds(a.dev_status); continue; }
@@ -182,8 +182,8 @@ __global__ void __launch_bounds__(kCommitThreads) commit_rows_kernel(const Commi
             if (a.acc_score) a.acc_score[(int64_t)hd * a.c.cap + ln + i] = 0.f;
             if (a.pos_cache) a.pos_cache[(int64_t)hd * a.c.cap + ln + i] = a.pos[(int64_t)b * a.draft_cap + j];
         }
-        x[u] = __ldg(reinterpret_cast<const uint4*>(a.Kd + src0 + (int64_t)j * kHeadDim) + ch);
-        y[u] = __ldg(reinterpret_cast<const uint4*>(a.Vd + src0 + (int64_t)j * kHeadDim) + ch);
+        x[u] = reinterpret_cast<const uint4*>(a.Kd + src0 + (int64_t)j * kHeadDim)[ch];
+        y[u] = reinterpret_cast<const uint4*>(a.Vd + src0 + (int64_t)j * kHeadDim)[ch];
     }
 #pragma unroll
     for (int u = 0; u < kCommitRows / kStep; ++u) {

@@ -7,16 +7,14 @@
 //
 // This kernel: tiles of 16 query rows on mma.sync.  A CTA is a producer warp and four compute warps around a ring of
 // stages of 64 keys, fetched by TMA tile copies (a box per page and 64 channels); a compute warp takes 16 keys of a stage.
-#include "cache.cuh"
 #include "exp2.cuh"
 #include "sm100.cuh"
+#include "tree_attn.cuh"
 
 namespace lvlm {
 
 using namespace sm100;
 
-constexpr int kTreeMaxT = 256;                       // drafts a sequence: eight mask words a row
-constexpr int kTreeMaxGroup = 64;
 constexpr int kTreeWarps = 4;
 constexpr int kTreeThreads = (kTreeWarps + 1) * 32;
 constexpr int kTreeRows = 16;                        // query rows a CTA
@@ -24,37 +22,13 @@ constexpr int kTreeStageKeys = 64;
 constexpr int kTreeBox = kTreeStageKeys * 128;       // 64 keys x 64 channels
 constexpr int kTreeStageBytes = 4 * kTreeBox;        // K low, K high, V low, V high channels
 constexpr int kTreeStages = 3;
-constexpr int kTreeTargetCtas = 2 * 148;
-constexpr float kTreeLog2e = 1.4426950408889634f, kTreeLn2 = 0.6931471805599453f;
+constexpr int kTreeTargetCtas = 2 * 148;             // CTAs wanted in flight: two an SM,
+constexpr int kTreeTcCtas = 148;                     // and one of the tcgen05 kernel
+constexpr int64_t kTreeMostSlots = 2 * kTreeTcCtas * kTreeTcRows;       // rows of partial results: two row tiles a CTA at most
+static_assert(kTreeMostSlots >= kTreeTargetCtas * kTreeRows, "");
 
-struct TreeArgs {
-    const __nv_bfloat16* q; const int32_t* table; const int32_t* len; const uint32_t* mask; const int32_t* count;
-    __nv_bfloat16* out; float* lse;
-    int B, H, G, T, W, drafts, mask_shared;          // W mask words a row; drafts = 0: no Kd
-    int S, row_tiles;
-    int64_t q_sb, q_sn, q_sh;
-    float scale_log2;
-    float2* part_ml;         // [head, row tile, part][row of the tile] (max in the log2 domain, sum)
-    float* part_o;           // [head, row tile, part][row of the tile][128] relative to that max
-    CacheGeom c;
-    int32_t* dev_status;
-};
-
-__device__ __forceinline__ void tree_flag(const TreeArgs& a, int bit) {
-    if (a.dev_status) atomicOr(a.dev_status, bit);
-}
-__device__ __forceinline__ int tree_count(const TreeArgs& a, int b) {
-    if (!a.count) return a.T;
-    const int n = __ldg(a.count + b);
-    if (n < 0 || n > a.T) { tree_flag(a, LVLM_DEV_BOUNDS); return 0; }
-    return n;
-}
-// The cache rows of a head, -1: its length is no length.
-__device__ __forceinline__ int tree_len(const TreeArgs& a, int hd) {
-    const int ln = __ldg(a.len + hd);
-    if (ln < 0 || ln > a.c.cap) { tree_flag(a, LVLM_DEV_BOUNDS); return -1; }
-    return ln;
-}
+// Which kernel.
+static bool tree_uses_tc(int64_t rows, int64_t) { return rows > kTreeRows; }
 
 __device__ __forceinline__ void tree_ldmatrix(uint32_t addr, uint32_t* r) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];\n"
@@ -137,7 +111,7 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                     if (a.c.page) {
                         // entries behind the head's length are not read: the last page of the head again
                         const int pg = min(j, ln - 1) >> a.c.shift;
-                        int id = __ldg(a.table + (int64_t)hd * a.c.max_pages + pg);
+                        int id = *(a.table + (int64_t)hd * a.c.max_pages + pg);
                         if (id < 0 || id >= a.c.n_pages) { tree_flag(a, LVLM_DEV_BOUNDS); id = a.c.n_pages; }   // the copy fills zeros there
                         c1 = j & (a.c.page - 1); c2 = id; c3 = 0;
                     }
@@ -154,22 +128,14 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             const int r = r0 + row + 8 * u, t = r / G, hh = r % G;
             qp[u] = r < rows ? reinterpret_cast<const uint32_t*>(a.q + (int64_t)b * a.q_sb + (int64_t)t * a.q_sn + (int64_t)(g * G + hh) * a.q_sh) : nullptr;
 #pragma unroll
-            for (int w = 0; w < kTreeMaxT / 32; ++w) {
-                uint32_t bits = 0;
-                if (r < rows && w < a.W && a.drafts) {
-                    if (a.mask) bits = __ldg(a.mask + ((int64_t)(a.mask_shared ? 0 : b) * T + t) * a.W + w);
-                    else bits = t >= w * 32 + 31 ? 0xFFFFFFFFu : t < w * 32 ? 0u : (2u << (t - w * 32)) - 1u;
-                    if (n < w * 32 + 32) bits &= n <= w * 32 ? 0u : (1u << (n - w * 32)) - 1u;
-                }
-                see[u][w] = bits;
-            }
+            for (int w = 0; w < kTreeMaxT / 32; ++w) see[u][w] = r < rows ? tree_see(a, b, t, n, w) : 0u;
         }
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks)
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                qa[ks][u] = qp[u] ? __ldg(qp[u] + ks * 8 + qd) : 0u;
-                qa[ks][2 + u] = qp[u] ? __ldg(qp[u] + ks * 8 + 4 + qd) : 0u;
+                qa[ks][u] = qp[u] ? *(qp[u] + ks * 8 + qd) : 0u;
+                qa[ks][2 + u] = qp[u] ? *(qp[u] + ks * 8 + 4 + qd) : 0u;
             }
         for (int i = 0; i < nstage; ++i) {
             const int s = i % kTreeStages, st = t_lo + i;
@@ -315,7 +281,7 @@ __global__ void __launch_bounds__(kTreeCombineThreads) tree_combine_kernel(const
     const int lane = threadIdx.x & 31, hd = blockIdx.y, b = hd / a.c.Hkv, g = hd % a.c.Hkv;
     const int r = blockIdx.x * (kTreeCombineThreads / 32) + (threadIdx.x >> 5);
     if (r >= tree_count(a, b) * a.G) return;
-    const int64_t rows = kTreeRows, at = ((int64_t)hd * a.row_tiles + r / kTreeRows) * a.S * kTreeRows + r % kTreeRows;
+    const int64_t rows = a.pitch, at = ((int64_t)hd * a.row_tiles + r / a.tile_rows) * a.S * a.pitch + r % a.tile_rows;
     float M = -INFINITY, Ls = 0.f;
     for (int p = lane; p < a.S; p += 32) M = fmaxf(M, a.part_ml[at + p * rows].x);
 #pragma unroll
@@ -336,29 +302,38 @@ __global__ void __launch_bounds__(kTreeCombineThreads) tree_combine_kernel(const
     if (a.lse && lane == 0) a.lse[((int64_t)b * a.H + h) * a.T + t] = Ls > 0.f ? (M + log2f(Ls)) * kTreeLn2 : -INFINITY;
 }
 
-// `total` is what a caller is told: room for as many parts as any problem of no more heads, rows and keys is cut into.
-struct TreeLayout { int S, row_tiles; size_t off_o, total; };
+// tc: the tcgen05 kernel.  `used`: bytes of workspace this call touches; `total` is what a caller is told: room for as many parts as any
+// problem of no more heads, rows and keys is cut into.
+struct TreeLayout { int tc, S, row_tiles, tile_rows, pitch; size_t off_o, used, total; };
 
 static bool tree_layout(const lvlm_dims* d, int64_t cap, TreeLayout* L) {
     if (d->B <= 0 || d->H <= 0 || d->Hkv <= 0 || d->H % d->Hkv || d->T <= 0 || d->T > kTreeMaxT || d->H / d->Hkv > kTreeMaxGroup || cap <= 0) return false;
-    const int64_t heads = (int64_t)d->B * d->Hkv, rows = (int64_t)d->T * (d->H / d->Hkv);
-    L->row_tiles = (int)((rows + kTreeRows - 1) / kTreeRows);
+    const int G = d->H / d->Hkv;
+    const int64_t heads = (int64_t)d->B * d->Hkv, rows = (int64_t)d->T * G;
     const int64_t keys = (d->N > 0 && d->N < cap ? d->N : cap) + (d->draft_cap > 0 ? d->T : 0);
-    const int64_t stages = (keys + kTreeStageKeys - 1) / kTreeStageKeys, tiles = heads * L->row_tiles;
-    int64_t S = kTreeTargetCtas / tiles;
-    S = S < 1 ? 1 : S > stages ? stages : S;
+    L->tc = tree_uses_tc(rows, keys);
+    L->pitch = L->tc ? kTreeTcRows : kTreeRows;
+    L->tile_rows = L->tc ? kTreeTcRows / G * G : kTreeRows;
+    L->row_tiles = (int)((rows + L->tile_rows - 1) / L->tile_rows);
+    const int64_t units = heads * (L->tc ? (L->row_tiles + 1) / 2 : L->row_tiles);       // CTAs where nothing is cut
+    const int64_t steps = (keys + (L->tc ? kTreeTcRows : kTreeStageKeys) - 1) / (L->tc ? kTreeTcRows : kTreeStageKeys);
+    int64_t S = (L->tc ? kTreeTcCtas : kTreeTargetCtas) / units;
+    S = S < 1 ? 1 : S > steps ? steps : S;
     L->S = (int)S;
-    const int64_t ctas = stages == 1 ? 0 : tiles * stages < kTreeTargetCtas ? tiles * stages : kTreeTargetCtas;
-    L->off_o = align_up((size_t)ctas * kTreeRows * 8, 256);
-    L->total = align_up(L->off_o + (size_t)ctas * kTreeRows * kHeadDim * 4, 256);
+    const int64_t slots = S > 1 ? heads * L->row_tiles * S * L->pitch : 0;
+    L->off_o = align_up((size_t)slots * 8, 256);
+    L->used = L->off_o + (size_t)slots * kHeadDim * 4;
+    const int64_t tc_tile = kTreeTcRows / G * G, stages = (keys + kTreeStageKeys - 1) / kTreeStageKeys;
+    const int64_t tc_rows = (rows + tc_tile - 1) / tc_tile * kTreeTcRows, mma_rows = (rows + kTreeRows - 1) / kTreeRows * kTreeRows;
+    const int64_t most = heads * (tc_rows > mma_rows ? tc_rows : mma_rows) * stages;
+    L->total = align_up((size_t)(most < kTreeMostSlots ? most : kTreeMostSlots) * (8 + kHeadDim * 4) + 256, 256);
     return true;
 }
 
 size_t tree_attn_workspace(const lvlm_dims* d) {
     TreeLayout L;
     const int64_t cap = d->page > 0 ? (int64_t)d->page * d->max_pages : d->cap;
-    if (!tree_layout(d, cap, &L)) return 0;
-    return L.total > 256 ? L.total : 256;
+    return tree_layout(d, cap, &L) ? L.total : 0;
 }
 
 }  // namespace lvlm
@@ -388,36 +363,45 @@ extern "C" lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void*
     if (!tree_layout(d, a.c.cap, &L)) return LVLM_ERR_INVALID_ARG;
     if (L.S > 1 && (!ws || !aligned256(ws) || ws_bytes < L.total)) return LVLM_ERR_WORKSPACE;
     char* wsb = static_cast<char*>(ws);
-    CUtensorMap kmap, vmap, kdmap, vdmap;
+    TreeMaps m;
     {
         const bool paged = a.c.page > 0;
+        const int box_rows = L.tc ? kTreeTcRows : kTreeStageKeys;
         const uint64_t dims[4] = {(uint64_t)kHeadDim, (uint64_t)(paged ? a.c.page : a.c.cap), (uint64_t)(paged ? a.c.n_pages : d->Hkv), (uint64_t)(paged ? 1 : d->B)};
         const uint64_t strides[3] = {(uint64_t)kHeadDim * 2, (uint64_t)a.c.sh * 2, (uint64_t)(paged ? a.c.sh : a.c.sb) * 2};
-        const uint32_t box[4] = {64, (uint32_t)(paged && a.c.page < kTreeStageKeys ? a.c.page : kTreeStageKeys), 1, 1};
-        if (!make_tmap_bf16(&kmap, Kc, 4, dims, strides, box) || !make_tmap_bf16(&vmap, Vc, 4, dims, strides, box)) return LVLM_ERR_CUDA;
-    }
-    if (Kd) {
-        const uint64_t dims[4] = {(uint64_t)kHeadDim, (uint64_t)d->T, (uint64_t)d->Hkv, (uint64_t)d->B};
-        const uint64_t strides[3] = {(uint64_t)kHeadDim * 2, (uint64_t)d_sh * 2, (uint64_t)d_sb * 2};
-        const uint32_t box[4] = {64, (uint32_t)kTreeStageKeys, 1, 1};
-        if (!make_tmap_bf16(&kdmap, Kd, 4, dims, strides, box) || !make_tmap_bf16(&vdmap, Vd, 4, dims, strides, box)) return LVLM_ERR_CUDA;
-    } else {
-        kdmap = kmap; vdmap = vmap;                             // not read
+        const uint32_t box[4] = {64, (uint32_t)(paged && a.c.page < box_rows ? a.c.page : box_rows), 1, 1};
+        if (!make_tmap_bf16(&m.k, Kc, 4, dims, strides, box) || !make_tmap_bf16(&m.v, Vc, 4, dims, strides, box)) return LVLM_ERR_CUDA;
+        m.kd = m.k; m.vd = m.v;                                 // without drafts: not read
+        if (Kd) {
+            const uint64_t ddims[4] = {(uint64_t)kHeadDim, (uint64_t)d->T, (uint64_t)d->Hkv, (uint64_t)d->B};
+            const uint64_t dstr[3] = {(uint64_t)kHeadDim * 2, (uint64_t)d_sh * 2, (uint64_t)d_sb * 2};
+            const uint32_t dbox[4] = {64, (uint32_t)box_rows, 1, 1};
+            if (!make_tmap_bf16(&m.kd, Kd, 4, ddims, dstr, dbox) || !make_tmap_bf16(&m.vd, Vd, 4, ddims, dstr, dbox)) return LVLM_ERR_CUDA;
+        }
     }
     a.q = static_cast<const __nv_bfloat16*>(q);
     a.table = table; a.len = len; a.mask = mask; a.count = count;
     a.out = static_cast<__nv_bfloat16*>(out); a.lse = lse;
     a.B = d->B; a.H = d->H; a.G = d->H / d->Hkv; a.T = d->T; a.W = (d->T + 31) / 32; a.drafts = Kd != nullptr; a.mask_shared = d->mask_shared != 0;
-    a.S = L.S; a.row_tiles = L.row_tiles;
+    a.S = L.S; a.row_tiles = L.row_tiles; a.tile_rows = L.tile_rows; a.pitch = L.pitch;
     a.scale_log2 = scale * kTreeLog2e;
     a.part_ml = reinterpret_cast<float2*>(wsb);
     a.part_o = reinterpret_cast<float*>(wsb + L.off_o);
     a.dev_status = dev_status;
     const int64_t heads = (int64_t)d->B * d->Hkv, ctas = heads * L.row_tiles * L.S;
-    if (ctas > 0x7FFFFFFFll || heads > 65535) return LVLM_ERR_UNSUPPORTED;
-    const size_t smem = 1024 + (size_t)kTreeStages * kTreeStageBytes;
-    LVLM_RETURN_IF_CUDA(cudaFuncSetAttribute(tree_mma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynSmem));
-    const lvlm_status st = launch_kernel(tree_mma_kernel, dim3((unsigned)ctas), dim3(kTreeThreads), smem, stream, 1, kmap, vmap, kdmap, vdmap, a);
+    if (ctas > 0x7FFFFFFFll) return LVLM_ERR_UNSUPPORTED;
+    lvlm_status st;
+    if (L.tc) {
+        const uint64_t dims[5] = {(uint64_t)kHeadDim, (uint64_t)a.G, (uint64_t)d->T, (uint64_t)d->Hkv, (uint64_t)d->B};
+        const uint64_t strides[4] = {(uint64_t)a.q_sh * 2, (uint64_t)a.q_sn * 2, (uint64_t)a.G * a.q_sh * 2, (uint64_t)a.q_sb * 2};
+        const uint32_t box[5] = {64, (uint32_t)a.G, (uint32_t)(kTreeTcRows / a.G), 1, 1};
+        if (!make_tmap_bf16(&m.q, q, 5, dims, strides, box)) return LVLM_ERR_CUDA;
+        st = launch_tree_tc(a, m, stream);
+    } else {
+        const size_t smem = 1024 + (size_t)kTreeStages * kTreeStageBytes;
+        LVLM_RETURN_IF_CUDA(cudaFuncSetAttribute(tree_mma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynSmem));
+        st = launch_kernel(tree_mma_kernel, dim3((unsigned)ctas), dim3(kTreeThreads), smem, stream, 1, m.k, m.v, m.kd, m.vd, a);
+    }
     if (st != LVLM_OK || L.S == 1) return st;
     const int rows = d->T * a.G, per = kTreeCombineThreads / 32;
     return launch_kernel(tree_combine_kernel, dim3((unsigned)((rows + per - 1) / per), (unsigned)heads), dim3(kTreeCombineThreads), 0, stream, 1, a);
