@@ -346,54 +346,93 @@ def decode_attn_static(q, Kc, Vc, length, *, k_new=None, v_new=None, acc_score=N
 _BF16, _I32, _F32 = torch.bfloat16, torch.int32, torch.float32
 
 
-def _arg(t: Optional[torch.Tensor], name: str, dtype, shape, device, last_packed_only=False) -> Optional[int]:
-    """Pointer of an optional argument after the checks that the C call cannot make."""
-    if t is None:
-        return None
+def _refuse(t: torch.Tensor, name: str, dtype, shape, device: int, rows: bool):
+    """Says what is wrong with an argument."""
     if not t.is_cuda:
         raise TypeError("lvlm works on CUDA tensors only; there is no CPU path")
     if t.dtype != dtype:
         raise TypeError(f"{name} has to be {dtype}, not {t.dtype}")
-    if t.device != device:
-        raise ValueError(f"{name} is on {t.device}, the other tensors on {device}")
+    if t.get_device() != device:
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{device}")
     if shape is not None and t.shape != shape:
         raise ValueError(f"{name} has to have the shape {tuple(shape)}, not {tuple(t.shape)}")
-    if t.stride(-1) != 1 and t.shape[-1] > 1 if last_packed_only else not t.is_contiguous():
-        raise ValueError(f"{name} has to be " + ("contiguous in its last dimension" if last_packed_only else "contiguous"))
+    raise ValueError(f"{name} has to be " + ("contiguous in its last dimension" if rows else "contiguous"))
+
+
+# One comparison an argument on the way through: a call of lvlm_rope_append spends 5 us of host time in its launch.
+def _arg(t: Optional[torch.Tensor], name: str, dtype, shape, device: int):
+    """Pointer of an optional contiguous argument after the checks that the C call cannot make."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.get_device() != device or (shape is not None and t.shape != shape) or not t.is_contiguous():
+        _refuse(t, name, dtype, shape, device, False)
     return t.data_ptr()
 
 
-def _strides(t: torch.Tensor, name: str, n: int):
+def _rows(t: torch.Tensor, name: str, shape, strides, device: int):
+    """Pointer of a bf16 argument of which only the rows of D channels have to be contiguous."""
+    if t.dtype is not _BF16 or t.get_device() != device or (shape is not None and t.shape != shape) or strides[-1] != 1:
+        _refuse(t, name, _BF16, shape, device, True)
+    return t.data_ptr()
+
+
+def _outer(t: torch.Tensor, name: str, strides, n: int):
     """The first n strides for the C call: 0 (packed) for a dimension of one element, whose stride means nothing."""
-    st = tuple(x if size > 1 else 0 for x, size in zip(t.stride()[:n], t.shape))
+    lead = strides[:n]
+    odd = 0
+    for x in lead:
+        odd |= x & 7 if x else 7
+    if not odd:
+        return lead
+    st = tuple([x if size > 1 else 0 for x, size in zip(strides[:n], t.shape)])
     if any(x == 0 and size > 1 for x, size in zip(st, t.shape)):
         raise ValueError(f"{name} repeats its elements along a dimension (an expanded view)")
     return st
 
 
-def _device(t: torch.Tensor) -> torch.device:
-    if t.is_cuda and t.device.index != torch.cuda.current_device():
-        raise ValueError(f"the tensors are on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    return t.device
-
-
-def _cache(d: Dims, Kc, Vc, table, B, Hkv, device):
+def _cache(d: Dims, Kc, Vc, table, B, Hkv, D, device: int):
     """Fills the cache's fields of ``d``; returns the three pointers."""
-    kp = _arg(Kc, "Kc", _BF16, None, device, True)
-    vp = _arg(Vc, "Vc", _BF16, Kc.shape, device, True)
-    if Vc.stride() != Kc.stride() or Kc.stride(-2) != Kc.shape[-1] and Kc.shape[-2] > 1:
+    st, shape = Kc.stride(), tuple(Kc.shape)
+    kp, vp = _rows(Kc, "Kc", None, st, device), _rows(Vc, "Vc", shape, st, device)
+    if Vc.stride() != st or st[-2] != shape[-1] and shape[-2] > 1:
         raise ValueError("Kc and Vc have to have the same strides and packed rows")
+    if shape[-1] != D:
+        raise ValueError(f"Kc has rows of {shape[-1]} channels, the new tokens of {D}")
     if table is None:
-        if Kc.dim() != 4 or Kc.shape[0] != B or Kc.shape[1] != Hkv:
-            raise ValueError(f"a contiguous cache has the shape [{B}, {Hkv}, cap, D], not {tuple(Kc.shape)}")
-        d.cap, d.D = Kc.shape[2], Kc.shape[3]
-        d.kv_stride_b, d.kv_stride_h = _strides(Kc, "Kc", 2)
+        if len(shape) != 4 or shape[0] != B or shape[1] != Hkv:
+            raise ValueError(f"a contiguous cache has the shape [{B}, {Hkv}, cap, D], not {tuple(shape)}")
+        d.cap = shape[2]
+        d.kv_stride_b, d.kv_stride_h = _outer(Kc, "Kc", st, 2)
         return kp, vp, None
-    if Kc.dim() != 3 or table.dim() != 3:
+    t_shape = table.shape
+    if len(shape) != 3 or len(t_shape) != 3:
         raise ValueError("a paged cache has the shape [n_pages, page, D], its table [B, Hkv, max_pages]")
-    d.n_pages, d.page, d.D = Kc.shape
-    (d.page_stride,), d.max_pages = _strides(Kc, "Kc", 1), table.shape[2]
-    return kp, vp, _arg(table, "table", _I32, (B, Hkv, d.max_pages), device)
+    d.n_pages, d.page, _ = shape
+    page_stride = st[0]
+    d.page_stride = page_stride if page_stride and not page_stride & 7 else _outer(Kc, "Kc", st, 1)[0]
+    d.max_pages = n = t_shape[2]
+    return kp, vp, _arg(table, "table", _I32, (B, Hkv, n), device)
+
+
+def _drafts(d: Dims, Kd, Vd, shape, device: int):
+    """The same for a draft cache [B,Hkv,draft_cap,D]."""
+    st = Kd.stride()
+    kp = _rows(Kd, "Kd", shape, st, device)
+    if Vd is None:
+        raise ValueError("Kd without Vd")
+    vp = _rows(Vd, "Vd", shape, st, device)
+    if Vd.stride() != st or st[2] != shape[3] and shape[2] > 1:
+        raise ValueError("Kd and Vd have to have the same strides and packed rows")
+    d.draft_cap = shape[2]
+    d.draft_stride_b, d.draft_stride_h = _outer(Kd, "Kd", st, 2)
+    return kp, vp
+
+
+def _here(t: torch.Tensor) -> int:
+    """The current device, on which every tensor has to be."""
+    if not t.is_cuda:
+        raise TypeError("lvlm works on CUDA tensors only; there is no CPU path")
+    return torch._C._cuda_getDevice()
 
 
 def rope_table(n_pos: int, rot: int = 128, base: float = 10000.0, device="cuda") -> torch.Tensor:
@@ -429,44 +468,51 @@ def rope_append(k_new, v_new, pos, cos_sin, Kc, Vc, length=None, *, q=None, q_ou
     into ``len_out``.  length None: the rows start at 0 (a draft cache), and no length is written unless len_out is given.
     pos is [B,T], or [3,B,T] with ``sections`` (the frequencies that follow each axis); cos_sin None: nothing is rotated.
     Returns q_out [B,T,H,D] (``q_out=q`` rotates in place) or None without q."""
-    dev = _device(k_new)
-    B, T, Hkv, D = k_new.shape
-    d = Dims(B=B, Hkv=Hkv, T=T, interleaved=int(interleaved))
-    kp, vp, tp = _cache(d, Kc, Vc, table, B, Hkv, dev)
-    if d.D != D:
-        raise ValueError(f"Kc has rows of {d.D} channels, k_new of {D}")
-    knp = _arg(k_new, "k_new", _BF16, None, dev, True)
-    vnp = _arg(v_new, "v_new", _BF16, k_new.shape, dev, True)
-    if v_new.stride() != k_new.stride():
+    dev = _here(k_new)
+    shape, st = tuple(k_new.shape), k_new.stride()
+    B, T, Hkv, D = shape
+    d = Dims()
+    d.B, d.Hkv, d.D, d.T, d.interleaved = B, Hkv, D, T, bool(interleaved)
+    kp, vp, tp = _cache(d, Kc, Vc, table, B, Hkv, D, dev)
+    knp, vnp = _rows(k_new, "k_new", None, st, dev), _rows(v_new, "v_new", shape, st, dev)
+    if v_new.stride() != st:
         raise ValueError("k_new and v_new have to have the same strides")
-    d.new_stride_b, d.new_stride_n, d.new_stride_h = _strides(k_new, "k_new", 3)
+    d.new_stride_b, d.new_stride_n, d.new_stride_h = _outer(k_new, "k_new", st, 3)
     qp = qop = None
     if q is not None:
-        H = q.shape[2]
-        qp = _arg(q, "q", _BF16, (B, T, H, D), dev, True)
-        d.H = H
-        d.q_stride_b, d.q_stride_n, d.q_stride_h = _strides(q, "q", 3)
-        if q_out is None:
-            q_out = torch.empty(B, T, H, D, dtype=_BF16, device=dev)
-        qop = q.data_ptr() if q_out is q else _arg(q_out, "q_out", _BF16, q.shape, dev)
-        if qop == qp and q_out.stride() != q.stride():
-            raise ValueError("q_out starts where q does but is laid out differently")
+        d.H = H = q.shape[2]
+        q_st, q_shape = q.stride(), (B, T, H, D)
+        qp = _rows(q, "q", q_shape, q_st, dev)
+        d.q_stride_b, d.q_stride_n, d.q_stride_h = _outer(q, "q", q_st, 3)
+        if q_out is q:
+            qop = qp
+        else:
+            if q_out is None:
+                q_out = torch.empty(B, T, H, D, dtype=_BF16, device=q.device)
+            qop = _arg(q_out, "q_out", _BF16, q_shape, dev)
+            if qop == qp and q_out.stride() != q_st:
+                raise ValueError("q_out starts where q does but is laid out differently")
+    elif q_out is not None:
+        raise ValueError("q_out without q")
     if cos_sin is not None:
         d.n_pos, d.rot = cos_sin.shape
+    pos_shape = (B, T)
     if sections is not None:
-        d.axes, d.sect0, d.sect1 = 3, sections[0], sections[1]
         if len(sections) != 3 or sum(sections) != d.rot // 2:
             raise ValueError(f"sections {tuple(sections)} do not share out {d.rot // 2} frequencies")
-    if len_out is None:
-        len_out = length
+        d.axes, d.sect0, d.sect1 = 3, sections[0], sections[1]
+        pos_shape = (3, B, T)
     hs = (B, Hkv)
-    side = (B, Hkv, d.cap or d.page * d.max_pages)
+    lp = _arg(length, "length", _I32, hs, dev)
+    ap = pcp = None
+    if acc_score is not None or pos_cache is not None:
+        side = (B, Hkv, d.cap or d.page * d.max_pages)
+        ap, pcp = _arg(acc_score, "acc_score", _F32, side, dev), _arg(pos_cache, "pos_cache", _I32, side, dev)
     _check(lib().lvlm_rope_append(
-        qp, knp, vnp, _arg(pos, "pos", _I32, (3, B, T) if sections is not None else (B, T), dev), _arg(cos_sin, "cos_sin", _F32, None, dev),
-        _arg(count, "count", _I32, (B,), dev), qop, kp, vp, tp, _arg(length, "length", _I32, hs, dev), _arg(len_out, "len_out", _I32, hs, dev),
-        _arg(acc_score, "acc_score", _F32, side, dev), _arg(pos_cache, "pos_cache", _I32, side, dev), ctypes.byref(d),
-        _arg(dev_status, "dev_status", _I32, None, dev), _stream(stream)), "lvlm_rope_append")
-    return q_out if q is not None else None
+        qp, knp, vnp, _arg(pos, "pos", _I32, pos_shape, dev), _arg(cos_sin, "cos_sin", _F32, None, dev),
+        _arg(count, "count", _I32, (B,), dev), qop, kp, vp, tp, lp, lp if len_out is None else _arg(len_out, "len_out", _I32, hs, dev),
+        ap, pcp, ctypes.byref(d), _arg(dev_status, "dev_status", _I32, None, dev), _stream(stream)), "lvlm_rope_append")
+    return q_out
 
 
 def commit_rows(Kd, Vd, Kc, Vc, length, count=None, *, index=None, table=None, len_out=None, pos=None, acc_score=None,
@@ -474,28 +520,25 @@ def commit_rows(Kd, Vd, Kc, Vc, length, count=None, *, index=None, table=None, l
     """lvlm_commit_rows.  Rows index[b,i] of Kd, Vd [B,Hkv,draft_cap,D] are appended to a cache behind ``length`` [B,Hkv], which
     grows by ``count``: in place, or into ``len_out``.  count [B] (None = all) or, to move a ragged cache, [B,Hkv];
     index [B,T] int32, None = the first rows."""
-    dev = _device(Kd)
-    B, Hkv, rows, D = Kd.shape
+    dev = _here(Kd)
+    shape = tuple(Kd.shape)
+    B, Hkv, rows, D = shape
     T = rows if index is None else index.shape[-1]
-    d = Dims(B=B, Hkv=Hkv, T=T, draft_cap=rows)
-    kp, vp, tp = _cache(d, Kc, Vc, table, B, Hkv, dev)
-    if d.D != D:
-        raise ValueError(f"Kc has rows of {d.D} channels, Kd of {D}")
-    kdp = _arg(Kd, "Kd", _BF16, None, dev, True)
-    vdp = _arg(Vd, "Vd", _BF16, Kd.shape, dev, True)
-    if Vd.stride() != Kd.stride() or Kd.stride(2) != D and rows > 1:
-        raise ValueError("Kd and Vd have to have the same strides and packed rows")
-    d.draft_stride_b, d.draft_stride_h = _strides(Kd, "Kd", 2)
+    d = Dims()
+    d.B, d.Hkv, d.D, d.T = B, Hkv, D, T
+    kp, vp, tp = _cache(d, Kc, Vc, table, B, Hkv, D, dev)
+    kdp, vdp = _drafts(d, Kd, Vd, shape, dev)
     hs = (B, Hkv)
-    d.count_heads = int(count is not None and count.dim() == 2)
-    side = (B, Hkv, d.cap or d.page * d.max_pages)
-    if len_out is None:
-        len_out = length
+    d.count_heads = count is not None and count.dim() == 2
+    lp = _arg(length, "length", _I32, hs, dev)
+    ap = pcp = None
+    if acc_score is not None or pos_cache is not None:
+        side = (B, Hkv, d.cap or d.page * d.max_pages)
+        ap, pcp = _arg(acc_score, "acc_score", _F32, side, dev), _arg(pos_cache, "pos_cache", _I32, side, dev)
     _check(lib().lvlm_commit_rows(
         kdp, vdp, _arg(index, "index", _I32, (B, T), dev), _arg(count, "count", _I32, hs if d.count_heads else (B,), dev),
-        _arg(pos, "pos", _I32, (B, rows), dev), kp, vp, tp, _arg(length, "length", _I32, hs, dev), _arg(len_out, "len_out", _I32, hs, dev),
-        _arg(acc_score, "acc_score", _F32, side, dev), _arg(pos_cache, "pos_cache", _I32, side, dev), ctypes.byref(d),
-        _arg(dev_status, "dev_status", _I32, None, dev), _stream(stream)), "lvlm_commit_rows")
+        _arg(pos, "pos", _I32, (B, rows), dev), kp, vp, tp, lp, lp if len_out is None else _arg(len_out, "len_out", _I32, hs, dev),
+        ap, pcp, ctypes.byref(d), _arg(dev_status, "dev_status", _I32, None, dev), _stream(stream)), "lvlm_commit_rows")
 
 
 def tree_dims(q, Kc, table=None, Kd=None, *, max_len=None) -> Dims:
@@ -517,36 +560,37 @@ def tree_attn(q, Kc, Vc, length, *, Kd=None, Vd=None, mask=None, count=None, tab
     drafts Kd, Vd [B,Hkv,>=T,D] that ``mask`` lets it see ([B,T,W] or [T,W] int32 words from ``tree_mask``; None = a chain).  count
     [B]: drafts of each sequence (None = T).  max_len: rows a head is expected to hold at most, where the caller knows (it decides
     how the work is split, not the result).  Returns (out [B,T,H,D], lse [B,H,T] or None); rows behind count are left as they were."""
-    dev = _device(q)
-    B, T, H, D = q.shape
-    d = tree_dims(q, Kc, table, Kd, max_len=max_len)
-    Hkv = d.Hkv
-    qp = _arg(q, "q", _BF16, None, dev, True)
-    d.q_stride_b, d.q_stride_n, d.q_stride_h = _strides(q, "q", 3)
-    kp, vp, tp = _cache(d, Kc, Vc, table, B, Hkv, dev)
-    if d.D != D:
-        raise ValueError(f"Kc has rows of {d.D} channels, q of {D}")
+    dev = _here(q)
+    shape, q_st = tuple(q.shape), q.stride()
+    B, T, H, D = shape
+    Hkv = Kc.shape[1] if table is None else table.shape[1]
+    d = Dims()
+    d.B, d.H, d.Hkv, d.D, d.T, d.N = B, H, Hkv, D, T, max_len or 0
+    qp = _rows(q, "q", None, q_st, dev)
+    d.q_stride_b, d.q_stride_n, d.q_stride_h = _outer(q, "q", q_st, 3)
+    kp, vp, tp = _cache(d, Kc, Vc, table, B, Hkv, D, dev)
     kdp = vdp = None
     if Kd is not None:
-        kdp = _arg(Kd, "Kd", _BF16, (B, Hkv, Kd.shape[2], D), dev, True)
-        vdp = _arg(Vd, "Vd", _BF16, Kd.shape, dev, True)
-        if Vd is not None and Vd.stride() != Kd.stride() or Kd.stride(2) != D and Kd.shape[2] > 1:
-            raise ValueError("Kd and Vd have to have the same strides and packed rows")
-        d.draft_stride_b, d.draft_stride_h = _strides(Kd, "Kd", 2)
+        kdp, vdp = _drafts(d, Kd, Vd, (B, Hkv, Kd.shape[2], D), dev)
+    elif Vd is not None:
+        raise ValueError("Vd without Kd")
     mp = None
     if mask is not None:
         W = (T + 31) // 32
-        d.mask_shared = int(mask.dim() == 2)
+        d.mask_shared = mask.dim() == 2
         mp = _arg(mask, "mask", _I32, (T, W) if d.mask_shared else (B, T, W), dev)
     if scale is None:
         scale = 1.0 / math.sqrt(D)
     if out is None:
-        out = torch.empty(B, T, H, D, dtype=_BF16, device=dev)
+        out = torch.empty(B, T, H, D, dtype=_BF16, device=q.device)
     if lse is None and want_lse:
-        lse = torch.empty(B, H, T, dtype=_F32, device=dev)
-    ws, wsp, wsn = _ws(ws, OP_TREE_ATTN, d, dev)
+        lse = torch.empty(B, H, T, dtype=_F32, device=q.device)
+    if ws is None:
+        ws = alloc_workspace(OP_TREE_ATTN, d, q.device)
+    elif ws.get_device() != dev:
+        raise ValueError(f"ws is on {ws.device}, the current device is cuda:{dev}")
     _check(lib().lvlm_tree_attn(qp, kp, vp, tp, _arg(length, "length", _I32, (B, Hkv), dev), kdp, vdp, mp,
-                                _arg(count, "count", _I32, (B,), dev), ctypes.byref(d), scale, _arg(out, "out", _BF16, (B, T, H, D), dev),
-                                _arg(lse, "lse", _F32, (B, H, T), dev), wsp, wsn, _arg(dev_status, "dev_status", _I32, None, dev),
-                                _stream(stream)), "lvlm_tree_attn")
+                                _arg(count, "count", _I32, (B,), dev), ctypes.byref(d), scale, _arg(out, "out", _BF16, shape, dev),
+                                _arg(lse, "lse", _F32, (B, H, T), dev), ws.data_ptr(), ws.numel() * ws.element_size(),
+                                _arg(dev_status, "dev_status", _I32, None, dev), _stream(stream)), "lvlm_tree_attn")
     return out, lse

@@ -1,12 +1,14 @@
 // lvlm_tree_attn: the drafted tokens of a sequence attend to its cache (contiguous or paged, ragged per KV head) and to one
 // another through a mask.
 //
-// For every (sequence, KV head) the T G query rows of the group (row r = token r / G, head r % G of the group) meet the
-// same keys: len cache rows, then the count drafts.  An online softmax runs over the keys; the keys of a head are cut into S runs
-// whose partial (max, sum, output) a second small launch adds in order.
+// For every (sequence, KV head) the T G query rows of the group (row r = draft r / G, head r % G of the group) meet the
+// same keys: len cache rows, then the count drafts.  An online softmax runs over the keys.
 //
-// This kernel: tiles of 16 query rows on mma.sync.  A CTA is a producer warp and four compute warps around a ring of
-// stages of 64 keys, fetched by TMA tile copies (a box per page and 64 channels); a compute warp takes 16 keys of a stage.
+// Few rows (tree_mma_kernel, here): a tile of 16 query rows on mma.sync.  The keys of a head are cut into runs for the CTAs of a
+// cluster.  A CTA is a producer warp and four compute warps around a ring of stages of 64 keys, fetched by TMA tile copies (a box per
+// page and 64 channels); a compute warp takes 16 keys of a stage.  The warps are added in shared memory, the CTAs of the cluster
+// through distributed shared memory: one launch, no workspace.
+// Many rows or keys: tree_tc.cu, on tcgen05; parts of a unit that it cut are added by tree_combine_kernel, here.
 #include "exp2.cuh"
 #include "sm100.cuh"
 #include "tree_attn.cuh"
@@ -22,13 +24,12 @@ constexpr int kTreeStageKeys = 64;
 constexpr int kTreeBox = kTreeStageKeys * 128;       // 64 keys x 64 channels
 constexpr int kTreeStageBytes = 4 * kTreeBox;        // K low, K high, V low, V high channels
 constexpr int kTreeStages = 3;
-constexpr int kTreeTargetCtas = 2 * 148;             // CTAs wanted in flight: two an SM,
-constexpr int kTreeTcCtas = 148;                     // and one of the tcgen05 kernel
-constexpr int64_t kTreeMostSlots = 2 * kTreeTcCtas * kTreeTcRows;       // rows of partial results: two row tiles a CTA at most
-static_assert(kTreeMostSlots >= kTreeTargetCtas * kTreeRows, "");
+constexpr int kTreeTargetCtas = 2 * 148;             // CTAs wanted in flight, two an SM
+constexpr int kTreeMaxCluster = 8;
+constexpr int kTreeMmaWords = 2;                     // mask words of a row: T <= 64
 
 // Which kernel.
-static bool tree_uses_tc(int64_t rows, int64_t) { return rows > kTreeRows; }
+static bool tree_uses_tc(int T, int64_t rows, int64_t) { return rows > kTreeRows || T > 32 * kTreeMmaWords; }
 
 __device__ __forceinline__ void tree_ldmatrix(uint32_t addr, uint32_t* r) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];\n"
@@ -52,14 +53,14 @@ __device__ __forceinline__ uint32_t tree_off(int r, int ch) {
     return (uint32_t)((ch >> 3) * kTreeBox + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
 }
 
-// grid.x = heads * row_tiles * S
+// grid.x = heads * row_tiles * S, clusters of S CTAs
 __global__ void __launch_bounds__(kTreeThreads, 2)
 tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
                 const __grid_constant__ CUtensorMap kdmap, const __grid_constant__ CUtensorMap vdmap, const TreeArgs a) {
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     __shared__ uint64_t s_full[kTreeStages], s_empty[kTreeStages];
-    __shared__ float2 s_ml[kTreeWarps][kTreeRows];
+    __shared__ float2 s_ml[kTreeWarps][kTreeRows], s_ML[kTreeRows];
     __shared__ int s_abort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
@@ -70,7 +71,7 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
     __syncthreads();
     pdl_enter();
     const int S = a.S, T = a.T, G = a.G, Hkv = a.c.Hkv;
-    const int part = blockIdx.x % S, tile = blockIdx.x / S % a.row_tiles, hd = blockIdx.x / S / a.row_tiles;
+    const int part = (int)cluster_ctarank(), tile = blockIdx.x / S % a.row_tiles, hd = blockIdx.x / S / a.row_tiles;
     const int b = hd / Hkv, g = hd % Hkv, r0 = tile * kTreeRows;
     const int n = tree_count(a, b), rows = n * G;               // rows behind `rows` are not asked for
     if (r0 >= rows) return;
@@ -94,41 +95,43 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
     };
     if (warp == kTreeWarps) {
         // ---- producer: lane i copies the i-th box of K and V halves of a stage ----------------------------------
-        const int box_rows = a.c.page ? min(a.c.page, kTreeStageKeys) : kTreeStageKeys;
+        const int box_rows = a.c.page ? min(a.c.page, kTreeStageKeys) : kTreeStageKeys, boxes = kTreeStageKeys / box_rows;    // 1, 2 or 4
+        const int quarter = lane & 3, bx = lane >> 2;
+        // the page of my box of stage st; entries behind the head's length are not read: its last page again
+        auto page_of = [&](int st) -> int {
+            if (!a.c.page || st >= ns || bx >= boxes) return 0;
+            return a.table[(int64_t)hd * a.c.max_pages + (min(st * kTreeStageKeys + bx * box_rows, ln - 1) >> a.c.shift)];
+        };
+        int id = page_of(t_lo);
         for (int i = 0; i < nstage; ++i) {
             const int s = i % kTreeStages, st = t_lo + i;
+            const int id_next = i + 1 < nstage ? page_of(st + 1) : 0;      // asked for a stage ahead
             if (i >= kTreeStages && !__all_sync(0xFFFFFFFFu, wait_on(&s_empty[s], (uint32_t)(i / kTreeStages - 1) & 1u))) break;
             if (lane == 0) mbar_arrive_expect_tx(&s_full[s], kTreeStageBytes);
             __syncwarp();
-            unsigned char* to = smem + s * kTreeStageBytes;
+            unsigned char* to = smem + s * kTreeStageBytes + quarter * kTreeBox;
             if (st >= ns) {
-                if (lane < 4) tma_load_4d(to + lane * kTreeBox, lane < 2 ? &kdmap : &vdmap, &s_full[s], (lane & 1) * 64, (st - ns) * kTreeStageKeys, g, b);
-            } else {
-                const int boxes = kTreeStageKeys / box_rows;    // 1, 2 or 4
-                if (lane < 4 * boxes) {
-                    const int part4 = lane & 3, bx = lane >> 2, j = st * kTreeStageKeys + bx * box_rows;
-                    int c1 = j, c2 = g, c3 = b;
-                    if (a.c.page) {
-                        // entries behind the head's length are not read: the last page of the head again
-                        const int pg = min(j, ln - 1) >> a.c.shift;
-                        int id = *(a.table + (int64_t)hd * a.c.max_pages + pg);
-                        if (id < 0 || id >= a.c.n_pages) { tree_flag(a, LVLM_DEV_BOUNDS); id = a.c.n_pages; }   // the copy fills zeros there
-                        c1 = j & (a.c.page - 1); c2 = id; c3 = 0;
-                    }
-                    tma_load_4d(to + part4 * kTreeBox + bx * box_rows * 128, part4 < 2 ? &kmap : &vmap, &s_full[s], (part4 & 1) * 64, c1, c2, c3);
+                if (lane < 4) tma_load_4d(to, quarter < 2 ? &kdmap : &vdmap, &s_full[s], (quarter & 1) * 64, (st - ns) * kTreeStageKeys, g, b);
+            } else if (bx < boxes) {
+                int c1 = st * kTreeStageKeys + bx * box_rows, c2 = g, c3 = b;
+                if (a.c.page) {
+                    if (id < 0 || id >= a.c.n_pages) { tree_flag(a, LVLM_DEV_BOUNDS); id = a.c.n_pages; }   // the copy fills zeros there
+                    c1 &= a.c.page - 1; c2 = id; c3 = 0;
                 }
+                tma_load_4d(to + bx * box_rows * 128, quarter < 2 ? &kmap : &vmap, &s_full[s], (quarter & 1) * 64, c1, c2, c3);
             }
+            id = id_next;
         }
     } else {
         uint32_t qa[8][4];
         const uint32_t* qp[2];
-        uint32_t see[2][kTreeMaxT / 32];                        // draft mask of my two rows
+        uint32_t see[2][kTreeMmaWords];                         // draft mask of my two rows
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int r = r0 + row + 8 * u, t = r / G, hh = r % G;
             qp[u] = r < rows ? reinterpret_cast<const uint32_t*>(a.q + (int64_t)b * a.q_sb + (int64_t)t * a.q_sn + (int64_t)(g * G + hh) * a.q_sh) : nullptr;
 #pragma unroll
-            for (int w = 0; w < kTreeMaxT / 32; ++w) see[u][w] = r < rows ? tree_see(a, b, t, n, w) : 0u;
+            for (int w = 0; w < kTreeMmaWords; ++w) see[u][w] = r < rows ? tree_see(a, b, t, n, w) : 0u;
         }
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks)
@@ -174,7 +177,7 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                         if (draft) {
                             uint32_t word = 0;
 #pragma unroll
-                            for (int w = 0; w < kTreeMaxT / 32; ++w) word = w == (j >> 5) ? see[u][w] : word;
+                            for (int w = 0; w < kTreeMmaWords; ++w) word = w == (j >> 5) ? see[u][w] : word;
                             vis = vis && ((word >> (j & 31)) & 1u);
                         }
                         sc[x][e] = vis ? sc[x][e] * a.scale_log2 : -INFINITY;
@@ -246,8 +249,7 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
     }
     __syncthreads();
     for (int idx = tid; idx < kTreeRows * (kHeadDim / 4); idx += kTreeThreads) {
-        const int rr = idx / (kHeadDim / 4), c4 = idx % (kHeadDim / 4), r = r0 + rr;
-        if (r >= rows) continue;
+        const int rr = idx / (kHeadDim / 4), c4 = idx % (kHeadDim / 4);
         float M = -INFINITY, Ls = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
@@ -260,73 +262,127 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             v.x += x.x * f; v.y += x.y * f; v.z += x.z * f; v.w += x.w * f;
             Ls += ml.y * f;
         }
-        if (S > 1) {
-            const int64_t at = (int64_t)blockIdx.x * kTreeRows + rr;
-            reinterpret_cast<float4*>(a.part_o + at * kHeadDim)[c4] = v;
-            if (c4 == 0) a.part_ml[at] = make_float2(M, Ls);
-        } else {
-            const int t = r / G, h = g * G + r % G;
-            const float inv = Ls > 0.f ? 1.0f / Ls : 0.f;
-            *reinterpret_cast<uint2*>(a.out + (((int64_t)b * T + t) * a.H + h) * kHeadDim + c4 * 4) =
-                make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
-            if (a.lse && c4 == 0) a.lse[((int64_t)b * a.H + h) * T + t] = Ls > 0.f ? (M + log2f(Ls)) * kTreeLn2 : -INFINITY;
+        *reinterpret_cast<float4*>(so + rr * kPitch + c4 * 4) = v;      // (over the first warp's, which only this thread reads)
+        if (c4 == 0) s_ML[rr] = make_float2(M, Ls);
+    }
+    // ---- the CTAs of the cluster, in rank order; a CTA finishes a slice of the rows and channels ---------------------------
+    cluster_barrier();
+    for (int idx = part * kTreeThreads + tid; idx < kTreeRows * (kHeadDim / 4); idx += S * kTreeThreads) {
+        const int rr = idx / (kHeadDim / 4), c4 = idx % (kHeadDim / 4), r = r0 + rr;
+        if (r >= rows) continue;
+        float2 ml[kTreeMaxCluster];
+        float4 x[kTreeMaxCluster];
+#pragma unroll
+        for (int c = 0; c < kTreeMaxCluster; ++c) {
+            ml[c] = make_float2(-INFINITY, 0.f);
+            x[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+            if (c < S) {
+                ml[c] = cluster_ld(&s_ML[rr], c);
+                x[c] = cluster_ld(reinterpret_cast<const float4*>(so + rr * kPitch + c4 * 4), c);
+            }
+        }
+        float M = -INFINITY, Ls = 0.f;
+        float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int c = 0; c < kTreeMaxCluster; ++c) M = fmaxf(M, ml[c].x);
+#pragma unroll
+        for (int c = 0; c < kTreeMaxCluster; ++c) {
+            const float f = ml[c].x > -INFINITY ? ex2_fast(ml[c].x - M) : 0.f;
+            v.x += x[c].x * f; v.y += x[c].y * f; v.z += x[c].z * f; v.w += x[c].w * f;
+            Ls += ml[c].y * f;
+        }
+        const int t = r / G, h = g * G + r % G;
+        const float inv = Ls > 0.f ? 1.0f / Ls : 0.f;
+        *reinterpret_cast<uint2*>(a.out + (((int64_t)b * T + t) * a.H + h) * kHeadDim + c4 * 4) =
+            make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
+        if (a.lse && c4 == 0) a.lse[((int64_t)b * a.H + h) * T + t] = Ls > 0.f ? (M + log2f(Ls)) * kTreeLn2 : -INFINITY;
+    }
+    cluster_arrive_exec();                                      // my reads of the other CTAs' shared memory are done
+    cluster_wait();                                             // and nobody leaves while its own is still read
+}
+
+// Adds the parts of a unit (a pair of row tiles of a head) that the tcgen05 kernel cut, in order.  Lane = row, a warp CH groups of four
+// channels of 32 rows: the loads are the lines that the parts were stored in.  grid (units, row blocks, channel blocks).
+constexpr int kTreeCombineWarps = 8;
+template <int CH>
+__global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(const TreeArgs a) {
+    pdl_enter();
+    const int pairs = (a.row_tiles + 1) / 2, lane = threadIdx.x & 31;
+    const int2 of = a.part_of[blockIdx.x];
+    const int hd = blockIdx.x / pairs, pair = blockIdx.x % pairs, b = hd / a.c.Hkv, g = hd % a.c.Hkv, tt = a.tile_rows / a.G;
+    const int place = blockIdx.y * 32 + lane, row = place % kTreeTcRows, tile = 2 * pair + place / kTreeTcRows;
+    const int n = tree_count(a, b);
+    if (2 * pair * tt >= n || of.x < 0) return;                 // nothing asked for, or not cut (of is only written where something is)
+    const int t = tile * tt + row / a.G;
+    const bool mine = row < a.tile_rows && t < n;
+    const int c0 = (blockIdx.z * kTreeCombineWarps + (threadIdx.x >> 5)) * CH, parts = of.y + 1;
+    // part p >= 1 lies in the first slot of its CTA
+    const int64_t rest = (int64_t)(of.x & ~1);
+    auto slot = [&](int p) -> int64_t { return p == 0 ? of.x : rest + 2 * p; };
+    float M = -INFINITY;
+#pragma unroll 4
+    for (int p = 0; p < parts; ++p) M = fmaxf(M, a.part_ml[slot(p) * a.pitch + place].x);
+    float4 v[CH];
+#pragma unroll
+    for (int c = 0; c < CH; ++c) v[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+    float Ls = 0.f;
+    constexpr int kAhead = 8 / CH;
+    for (int p0 = 0; p0 < parts; p0 += kAhead) {
+        float4 x[kAhead][CH];
+        float2 ml[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            ml[u] = make_float2(-INFINITY, 0.f);
+            if (p0 + u < parts) {
+                const int64_t s = slot(p0 + u);
+                ml[u] = a.part_ml[s * a.pitch + place];
+#pragma unroll
+                for (int c = 0; c < CH; ++c) x[u][c] = reinterpret_cast<const float4*>(a.part_o + s * a.pitch * kHeadDim)[(int64_t)(c0 + c) * a.pitch + place];
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            if (ml[u].x == -INFINITY) continue;
+            const float w = ex2_fast(ml[u].x - M);
+            Ls += ml[u].y * w;
+#pragma unroll
+            for (int c = 0; c < CH; ++c) { v[c].x += x[u][c].x * w; v[c].y += x[u][c].y * w; v[c].z += x[u][c].z * w; v[c].w += x[u][c].w * w; }
         }
     }
-}
-
-// Adds the S parts of a row in order.  A warp a row: a lane has four channels.
-constexpr int kTreeCombineThreads = 128;
-__global__ void __launch_bounds__(kTreeCombineThreads) tree_combine_kernel(const TreeArgs a) {
-    pdl_enter();
-    const int lane = threadIdx.x & 31, hd = blockIdx.y, b = hd / a.c.Hkv, g = hd % a.c.Hkv;
-    const int r = blockIdx.x * (kTreeCombineThreads / 32) + (threadIdx.x >> 5);
-    if (r >= tree_count(a, b) * a.G) return;
-    const int64_t rows = a.pitch, at = ((int64_t)hd * a.row_tiles + r / a.tile_rows) * a.S * a.pitch + r % a.tile_rows;
-    float M = -INFINITY, Ls = 0.f;
-    for (int p = lane; p < a.S; p += 32) M = fmaxf(M, a.part_ml[at + p * rows].x);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xFFFFFFFFu, M, o));
-    float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int p = 0; p < a.S; ++p) {
-        const float2 ml = a.part_ml[at + p * rows];
-        if (ml.x == -INFINITY) continue;
-        const float f = ex2_fast(ml.x - M);
-        const float4 x = reinterpret_cast<const float4*>(a.part_o + (at + p * rows) * kHeadDim)[lane];
-        v.x += x.x * f; v.y += x.y * f; v.z += x.z * f; v.w += x.w * f;
-        Ls += ml.y * f;
-    }
-    const int t = r / a.G, h = g * a.G + r % a.G;
+    if (!mine) return;
+    const int h = g * a.G + row % a.G;
     const float inv = Ls > 0.f ? 1.0f / Ls : 0.f;
-    *reinterpret_cast<uint2*>(a.out + (((int64_t)b * a.T + t) * a.H + h) * kHeadDim + lane * 4) =
-        make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
-    if (a.lse && lane == 0) a.lse[((int64_t)b * a.H + h) * a.T + t] = Ls > 0.f ? (M + log2f(Ls)) * kTreeLn2 : -INFINITY;
+    uint2* to = reinterpret_cast<uint2*>(a.out + (((int64_t)b * a.T + t) * a.H + h) * kHeadDim) + c0;
+#pragma unroll
+    for (int c = 0; c < CH; ++c) to[c] = make_uint2(pack_bf16(v[c].x * inv, v[c].y * inv), pack_bf16(v[c].z * inv, v[c].w * inv));
+    if (a.lse && c0 == 0) a.lse[((int64_t)b * a.H + h) * a.T + t] = Ls > 0.f ? (M + log2f(Ls)) * kTreeLn2 : -INFINITY;
 }
 
-// tc: the tcgen05 kernel.  `used`: bytes of workspace this call touches; `total` is what a caller is told: room for as many parts as any
-// problem of no more heads, rows and keys is cut into.
-struct TreeLayout { int tc, S, row_tiles, tile_rows, pitch; size_t off_o, used, total; };
+// tc: the tcgen05 kernel.  `total` is what a caller is told, whichever kernel it is, so that it never shrinks as a problem grows.
+struct TreeLayout { int tc, S, row_tiles, tile_rows, pitch; size_t off_o, off_of, total; };
 
 static bool tree_layout(const lvlm_dims* d, int64_t cap, TreeLayout* L) {
     if (d->B <= 0 || d->H <= 0 || d->Hkv <= 0 || d->H % d->Hkv || d->T <= 0 || d->T > kTreeMaxT || d->H / d->Hkv > kTreeMaxGroup || cap <= 0) return false;
     const int G = d->H / d->Hkv;
     const int64_t heads = (int64_t)d->B * d->Hkv, rows = (int64_t)d->T * G;
     const int64_t keys = (d->N > 0 && d->N < cap ? d->N : cap) + (d->draft_cap > 0 ? d->T : 0);
-    L->tc = tree_uses_tc(rows, keys);
-    L->pitch = L->tc ? kTreeTcRows : kTreeRows;
-    L->tile_rows = L->tc ? kTreeTcRows / G * G : kTreeRows;
+    const int64_t mma_tiles = heads * ((rows + kTreeRows - 1) / kTreeRows);
+    L->tc = tree_uses_tc(d->T, rows, keys);
+    // the tcgen05 kernel: CTAs by the work there is at most, two slots each
+    const int64_t tc_tile = kTreeTcRows / G * G, tc_tiles = (rows + tc_tile - 1) / tc_tile;
+    const int64_t work = heads * tc_tiles * ((keys + kTreeTcRows - 1) / kTreeTcRows + 1) / kTreeTcLeast;
+    const int64_t tc_S = work < 1 ? 1 : work > kTreeTcCtas ? kTreeTcCtas : work;
+    L->pitch = (tc_tiles > 1 ? 2 : 1) * kTreeTcRows;
+    const int64_t places = tc_S > 1 ? 2 * tc_S * L->pitch : 0;
+    L->off_o = align_up((size_t)places * 8, 256);
+    L->off_of = L->off_o + (size_t)places * kHeadDim * 4;
+    L->total = align_up(L->off_of + (size_t)(heads * ((tc_tiles + 1) / 2)) * 8, 256);
+    // the other: clusters as large as the GPU has room for, a CTA with a stage of keys at least
+    int S = 1;
+    while (S < kTreeMaxCluster && mma_tiles * 2 * S <= kTreeTargetCtas && keys >= 2 * S * kTreeStageKeys) S *= 2;
+    L->S = L->tc ? (int)tc_S : S;
+    L->tile_rows = L->tc ? (int)tc_tile : kTreeRows;
     L->row_tiles = (int)((rows + L->tile_rows - 1) / L->tile_rows);
-    const int64_t units = heads * (L->tc ? (L->row_tiles + 1) / 2 : L->row_tiles);       // CTAs where nothing is cut
-    const int64_t steps = (keys + (L->tc ? kTreeTcRows : kTreeStageKeys) - 1) / (L->tc ? kTreeTcRows : kTreeStageKeys);
-    int64_t S = (L->tc ? kTreeTcCtas : kTreeTargetCtas) / units;
-    S = S < 1 ? 1 : S > steps ? steps : S;
-    L->S = (int)S;
-    const int64_t slots = S > 1 ? heads * L->row_tiles * S * L->pitch : 0;
-    L->off_o = align_up((size_t)slots * 8, 256);
-    L->used = L->off_o + (size_t)slots * kHeadDim * 4;
-    const int64_t tc_tile = kTreeTcRows / G * G, stages = (keys + kTreeStageKeys - 1) / kTreeStageKeys;
-    const int64_t tc_rows = (rows + tc_tile - 1) / tc_tile * kTreeTcRows, mma_rows = (rows + kTreeRows - 1) / kTreeRows * kTreeRows;
-    const int64_t most = heads * (tc_rows > mma_rows ? tc_rows : mma_rows) * stages;
-    L->total = align_up((size_t)(most < kTreeMostSlots ? most : kTreeMostSlots) * (8 + kHeadDim * 4) + 256, 256);
     return true;
 }
 
@@ -361,7 +417,7 @@ extern "C" lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void*
         return LVLM_ERR_ALIGNMENT;
     TreeLayout L;
     if (!tree_layout(d, a.c.cap, &L)) return LVLM_ERR_INVALID_ARG;
-    if (L.S > 1 && (!ws || !aligned256(ws) || ws_bytes < L.total)) return LVLM_ERR_WORKSPACE;
+    if (!ws || !aligned256(ws) || ws_bytes < L.total) return LVLM_ERR_WORKSPACE;
     char* wsb = static_cast<char*>(ws);
     TreeMaps m;
     {
@@ -387,6 +443,7 @@ extern "C" lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void*
     a.scale_log2 = scale * kTreeLog2e;
     a.part_ml = reinterpret_cast<float2*>(wsb);
     a.part_o = reinterpret_cast<float*>(wsb + L.off_o);
+    a.part_of = reinterpret_cast<int2*>(wsb + L.off_of);
     a.dev_status = dev_status;
     const int64_t heads = (int64_t)d->B * d->Hkv, ctas = heads * L.row_tiles * L.S;
     if (ctas > 0x7FFFFFFFll) return LVLM_ERR_UNSUPPORTED;
@@ -400,9 +457,13 @@ extern "C" lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void*
     } else {
         const size_t smem = 1024 + (size_t)kTreeStages * kTreeStageBytes;
         LVLM_RETURN_IF_CUDA(cudaFuncSetAttribute(tree_mma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynSmem));
-        st = launch_kernel(tree_mma_kernel, dim3((unsigned)ctas), dim3(kTreeThreads), smem, stream, 1, m.k, m.v, m.kd, m.vd, a);
+        return launch_kernel(tree_mma_kernel, dim3((unsigned)ctas), dim3(kTreeThreads), smem, stream, L.S, m.k, m.v, m.kd, m.vd, a);
     }
     if (st != LVLM_OK || L.S == 1) return st;
-    const int rows = d->T * a.G, per = kTreeCombineThreads / 32;
-    return launch_kernel(tree_combine_kernel, dim3((unsigned)((rows + per - 1) / per), (unsigned)heads), dim3(kTreeCombineThreads), 0, stream, 1, a);
+    // a warp takes one group of channels where few units leave the GPU idle otherwise
+    const int64_t units = heads * ((L.row_tiles + 1) / 2);
+    const unsigned blocks = (unsigned)(L.pitch / 32);
+    if (units * blocks < 148)
+        return launch_kernel(tree_combine_kernel<1>, dim3((unsigned)units, blocks, 4), dim3(kTreeCombineWarps * 32), 0, stream, 1, a);
+    return launch_kernel(tree_combine_kernel<4>, dim3((unsigned)units, blocks, 1), dim3(kTreeCombineWarps * 32), 0, stream, 1, a);
 }

@@ -9,18 +9,24 @@ namespace lvlm {
 constexpr int kTreeMaxT = 256;                       // drafts a sequence: eight mask words a row
 constexpr int kTreeMaxGroup = 64;
 constexpr int kTreeTcRows = 128;                     // rows of a tile of the tcgen05 kernel
+constexpr int kTreeTcCtas = 148;                     // its CTAs, one an SM
+constexpr int kTreeTcLeast = 4;                      // least work of one, in key tiles of a row tile (2 or more)
 constexpr float kTreeLog2e = 1.4426950408889634f, kTreeLn2 = 0.6931471805599453f;
 
 struct TreeArgs {
     const __nv_bfloat16* q; const int32_t* table; const int32_t* len; const uint32_t* mask; const int32_t* count;
     __nv_bfloat16* out; float* lse;
     int B, H, G, T, W, drafts, mask_shared;          // W mask words a row; drafts = 0: no Kd
-    int S, row_tiles;        // runs a head's keys are cut into; tiles of its T G query rows
-    int tile_rows, pitch;    // query rows in a tile, and places for them in the workspace
+    int S, row_tiles;        // CTAs of a cluster (tcgen05 kernel: of the grid); tiles of its T G query rows
+    int tile_rows, pitch;    // query rows in a tile, and places for rows in a slot of the workspace
     int64_t q_sb, q_sn, q_sh;
     float scale_log2;
-    float2* part_ml;         // [head, row tile, part][pitch] (max in the log2 domain, sum)
-    float* part_o;           // [head, row tile, part][pitch][128] relative to that max
+    // Partial results of the tcgen05 kernel.  A slot holds `pitch` rows, groups of four channels of all rows side by side; a CTA has two slots,
+    // for its first segment and its last; part_of [head, pair of row tiles]: the first slot of a unit, -1 = it was not cut, and how
+    // many more CTAs have a part of it, in their first slots.
+    float2* part_ml;         // (max in the log2 domain, sum)
+    float* part_o;           // output relative to that max
+    int2* part_of;
     CacheGeom c;
     int32_t* dev_status;
 };

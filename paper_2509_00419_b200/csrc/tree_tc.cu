@@ -1,13 +1,16 @@
 // lvlm_tree_attn, many query rows or long caches: tcgen05.
 //
-// The T G query rows of a KV head lie in tiles of up to 128 rows, floor(128 / G) drafts with all heads of the group.  A CTA takes
-// a run of the head's key tiles (128 keys: the cache, then the drafts) for two row tiles that take turns at the tensor cores, or
-// for one row tile, whose key tiles the two halves of the CTA take in turn and whose results they add at the end:
+// The T G query rows of a KV head lie in tiles of up to 128 rows, floor(128 / G) drafts with all heads of the group.  A unit of work is
+// two row tiles of a head that take turns at the tensor cores against its key tiles (128 keys: the cache, then the drafts), or the odd
+// row tile out, whose key tiles the two halves of a CTA take in turn and whose results they add at the end:
 //   S = Q K_j^T      operands by TMA (128-byte swizzle; a box per page where the cache is paged), 128x128 fp32 in tensor memory
 //   softmax          thread = query row, running maximum and sum in the log2 domain; probabilities go back as bf16 head + bf16
 //                    remainder over the logits they came from (a plain bf16 would cost as much again as the rounding of the result)
 //   O += P V_j       A = P from tensor memory, B = V as it lies in memory
-// The keys of a head are cut into S runs, one CTA each, so that the grid fills the SMs; the parts are added by tree_combine_kernel.
+// One CTA an SM.  Lengths are ragged and only known on the device, so the key tiles of all units, weighted by what they take, are laid
+// end to end there and every CTA takes an equal run of them: a scheduler warp cuts the run into segments, a unit each, and the
+// other warps work through them without stopping in between (the keys of the next segment are fetched during the epilogue of this one).
+// A unit that is cut leaves its parts (max, sum, output) in the workspace; tree_combine_kernel adds them in order.
 // Rows of V behind the end of the cache or of the drafts are zeroed in shared memory before they are multiplied: they may hold
 // anything, and their weight of zero would not stop a NaN.
 #include "exp2.cuh"
@@ -29,23 +32,51 @@ static_assert(3 * kTRegsLaunch >= kTRegsFew + 2 * kTRegsMany, "the split has to 
 constexpr uint32_t kTTmemCols = 512;         // S/P of the two halves | O of the two halves
 constexpr float kTRescaleStep = 8.0f;
 
+// The key tiles and row tiles of a head; a head without keys has one tile of none, so that its rows are written.
+struct TreeHead { int n, ln, ns, nt, rt; };
+__device__ __forceinline__ TreeHead tree_head(const TreeArgs& a, int hd, int tt) {
+    const int ln = a.len[hd], n = a.count ? a.count[hd / a.c.Hkv] : a.T;      // (both on their way before either is looked at)
+    TreeHead h;
+    h.n = n < 0 || n > a.T ? 0 : n;
+    h.ln = ln < 0 || ln > a.c.cap ? -1 : ln;
+    if (h.n != n || h.ln != ln) tree_flag(a, LVLM_DEV_BOUNDS);
+    h.ns = h.ln > 0 ? (h.ln + kTT - 1) / kTT : 0;
+    h.nt = h.ln < 0 ? 0 : h.ns + (a.drafts ? (h.n + kTT - 1) / kTT : 0);
+    h.rt = h.n <= tt ? (h.n > 0) : (h.n + tt - 1) / tt;
+    return h;
+}
+// What a head weighs: a pair of row tiles 2 a key tile, an odd one 1.
+__device__ __forceinline__ int tree_weight(const TreeHead& h) { return max(h.nt, 1) * h.rt; }     // (far below 2^31: a tile is 64 KB)
+
+constexpr int kTSegs = 4;                    // segments the scheduler is ahead at most
+struct TreeSeg { int hd, pair, t0, nk, split, n, ln, slot; };      // key tiles t0 .. t0 + nk - 1 of a unit; slot < 0: all of them; hd < 0: the end
+
 struct TreeTcSmem {
+    uint64_t seg_full[kTSegs], seg_empty[kTSegs], e_done, x_ready;
+    TreeSeg seg[kTSegs];
+    long long scan[kTThreads / 32], first_prefix;
+    int first_head;
+    TreeHead first;
     uint64_t q_full, k_full[kTStages], k_empty[kTStages], v_full[kTStages], v_empty[kTStages], s_full[2], p_ready[2][2], o_done[2];
     uint32_t tmem_base;
     volatile int abort;
     float xm[2][kTT], xl[2][kTT];            // one row tile: (max, sum) of a row over the key tiles of either half
 };
 
+// One short loop: the kernel runs through most of its code once, so that code fetched is time spent.
 __device__ __forceinline__ bool tree_wait(uint64_t* bar, uint32_t parity, TreeTcSmem* sm, const TreeArgs& a) {
-    if (mbar_try(bar, parity)) return true;
-    if (sm->abort) return false;
-    if (mbar_wait(bar, parity)) return true;
+    const uint32_t addr = smem_u32(bar);
+#pragma unroll 1
+    for (uint32_t it = 0; it < kSpinLimit; ++it) {
+        if (mbar_try_for(addr, parity)) return true;
+        if (sm->abort) return false;
+    }
     sm->abort = 1;
     tree_flag(a, LVLM_DEV_TIMEOUT);
     return false;
 }
 
-// grid.x = heads * S * pairs of row tiles; the pairs of a head and run lie side by side, so that they read the keys from L2
+// grid.x = CTAs at most (one an SM)
 __global__ void __launch_bounds__(kTThreads, 1)
 tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
                const __grid_constant__ CUtensorMap kdmap, const __grid_constant__ CUtensorMap vdmap, const TreeArgs a) {
@@ -58,7 +89,8 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
     if (threadIdx.x == 0) {
-        mbar_init(&sm->q_full, 1);
+        mbar_init(&sm->q_full, 1); mbar_init(&sm->e_done, 8); mbar_init(&sm->x_ready, 8);
+        for (int s = 0; s < kTSegs; ++s) { mbar_init(&sm->seg_full[s], 1); mbar_init(&sm->seg_empty[s], 10); }
         for (int s = 0; s < kTStages; ++s) {
             mbar_init(&sm->k_full[s], 1); mbar_init(&sm->k_empty[s], 1);
             mbar_init(&sm->v_full[s], 1); mbar_init(&sm->v_empty[s], 1);
@@ -81,145 +113,270 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     const uint32_t tmem_base = sm->tmem_base;
     pdl_enter();
 
-    const int G = a.G, T = a.T, Hkv = a.c.Hkv, pairs = (a.row_tiles + 1) / 2;
-    const int pair = blockIdx.x % pairs, part = blockIdx.x / pairs % a.S, hd = blockIdx.x / pairs / a.S;
-    const int b = hd / Hkv, g = hd % Hkv, tt = kTT / G;          // drafts a row tile
-    const int n = tree_count(a, b), ln = tree_len(a, hd);
-    const int ns = ln > 0 ? (ln + kTT - 1) / kTT : 0;
-    const int nt = ln < 0 ? 0 : ns + (a.drafts ? (n + kTT - 1) / kTT : 0);
-    const int per = (nt + a.S - 1) / a.S, t_lo = min(nt, part * per);
-    // my row tiles 2 pair and, where it has rows that are asked for, 2 pair + 1
-    const bool any = 2 * pair * tt < n;
-    const int split = (2 * pair + 1) * tt >= n;                  // one row tile: its key tiles in turn
-    const int nk = any ? min(nt, t_lo + per) - t_lo : 0;         // my key tiles t_lo ..
-    const int nk2[2] = {split ? (nk + 1) / 2 : nk, split ? nk / 2 : nk};      // and of either half; its i-th is i, or with one row tile 2 i + u
+    // ---- my run [lo, hi) of the weights of all heads, and the head it begins in ------------------------------------
+    const int G = a.G, T = a.T, Hkv = a.c.Hkv, heads = a.B * Hkv, tt = kTT / G, me = blockIdx.x;      // tt drafts a row tile
+    const int each = (heads + kTThreads - 1) / kTThreads, h_lo = min(heads, (int)threadIdx.x * each), h_hi = min(heads, h_lo + each);
+    long long sum = 0;
+    TreeHead head;
+#pragma unroll 1
+    for (int hd = h_lo; hd < h_hi; ++hd) {
+        head = tree_head(a, hd, tt);
+        sum += tree_weight(head);
+    }
+    long long incl = sum;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const long long x = __shfl_up_sync(0xFFFFFFFFu, incl, o);
+        if (lane >= o) incl += x;
+    }
+    if (lane == 31) sm->scan[warp] = incl;
+    __syncthreads();
+    long long total = 0, before = incl - sum;
+#pragma unroll
+    for (int w = 0; w < kTThreads / 32; ++w) {
+        if (w < warp) before += sm->scan[w];
+        total += sm->scan[w];
+    }
+    // equal runs, none so short that it is not worth a CTA's start
+    const long long share = total >> 32 ? (total + gridDim.x - 1) / gridDim.x : (long long)(((uint32_t)total + gridDim.x - 1) / gridDim.x);
+    const long long per = max((long long)kTreeTcLeast, share), lo = min(total, per * me), hi = min(total, lo + per);
+    if (lo < hi && lo >= before && lo < before + sum) {
+        long long p = before;
+        int hd = h_lo;
+        if (each > 1)
+            for (;; ++hd) {
+                head = tree_head(a, hd, tt);
+                if (lo < p + tree_weight(head)) break;
+                p += tree_weight(head);
+            }
+        sm->first_head = hd;
+        sm->first_prefix = p;
+        sm->first = head;
+    }
+    __syncthreads();
+    // the s-th segment of my run, for every warp but the scheduler
+    auto segment = [&](int s) -> TreeSeg {
+        TreeSeg x;
+        x.hd = -1;
+        if (__all_sync(0xFFFFFFFFu, tree_wait(&sm->seg_full[s % kTSegs], (s / kTSegs) & 1, sm, a))) {
+            x = sm->seg[s % kTSegs];
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm->seg_empty[s % kTSegs]);
+        }
+        return x;
+    };
 
     if (warp < 4) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kTRegsFew));
-    if (warp == 0 && nk > 0) {
+    if (warp == 0) {
         // ================= TMA producer: lane 2 x + half copies the x-th page of a tile =================
-        if (lane == 0) {
-            const int nq = split ? 1 : 2;
-            mbar_arrive_expect_tx(&sm->q_full, (uint32_t)(nq * 2 * tt * G * 128));
-            for (int u = 0; u < nq; ++u) {
-                tma_load_5d(sQ + u * kTTile, &qmap, &sm->q_full, 0, 0, (2 * pair + u) * tt, g, b);
-                tma_load_5d(sQ + u * kTTile + kTHalf, &qmap, &sm->q_full, 64, 0, (2 * pair + u) * tt, g, b);
-            }
-        }
         const int box_rows = a.c.page ? min(a.c.page, kTT) : kTT, boxes = kTT / box_rows;
         const int half = lane & 1, x = lane >> 1;
-        // the page of my box of tile t; entries behind the head's length are not read: its last page again
-        auto page_of = [&](int t) -> int {
-            if (!a.c.page || t >= ns || x >= boxes) return 0;
-            const int pg = min(t * kTT + x * box_rows, ln - 1) >> a.c.shift;
-            return a.table[(int64_t)hd * a.c.max_pages + pg];
-        };
-        int id = page_of(t_lo);
-        for (int j = 0; j < nk; ++j) {
-            const int st = j % kTStages, t = t_lo + j;
-            const int id_next = j + 1 < nk ? page_of(t + 1) : 0;   // asked for a tile ahead
-            const bool draft = t >= ns;
-            int c1 = draft ? (t - ns) * kTT : t * kTT + x * box_rows, c2 = g, c3 = b;
-            if (!draft && a.c.page) {
-                if (id < 0 || id >= a.c.n_pages) { tree_flag(a, LVLM_DEV_BOUNDS); id = a.c.n_pages; }    // the copy fills zeros there
-                c1 &= a.c.page - 1; c2 = id; c3 = 0;
+        int kc = 0, qc = 0;                                       // tiles and query tiles fetched for the segments before
+        bool ok = true;
+#pragma unroll 1
+        for (int s = 0; ok; ++s) {
+            const TreeSeg w = segment(s);
+            if (w.hd < 0) break;
+            const int b = w.hd / Hkv, g = w.hd % Hkv, ns = w.ln > 0 ? (w.ln + kTT - 1) / kTT : 0;
+            // the page of my box of tile t; entries behind the head's length are not read: its last page again
+            auto page_of = [&](int t) -> int {
+                if (!a.c.page || t >= ns || x >= boxes) return 0;
+                const int pg = min(t * kTT + x * box_rows, w.ln - 1) >> a.c.shift;
+                return a.table[(int64_t)w.hd * a.c.max_pages + pg];
+            };
+            int id = page_of(w.t0), id_next = w.nk > 1 ? page_of(w.t0 + 1) : 0;      // asked for two tiles ahead
+            // the queries: behind the first keys, once the epilogue of the segment before has left their place
+            const int q_at = w.nk == 0 ? -1 : qc == 0 ? 0 : min(kTStages, w.nk);
+#pragma unroll 1
+            for (int j = 0; j <= w.nk; ++j) {
+                if (j == q_at) {
+                    ok = qc == 0 || __all_sync(0xFFFFFFFFu, tree_wait(&sm->e_done, (qc - 1) & 1, sm, a));
+                    if (!ok) break;
+                    if (lane == 0) {
+                        const int nq = w.split ? 1 : 2;
+                        mbar_arrive_expect_tx(&sm->q_full, (uint32_t)(nq * 2 * tt * G * 128));
+                        for (int u = 0; u < nq; ++u) {
+                            tma_load_5d(sQ + u * kTTile, &qmap, &sm->q_full, 0, 0, (2 * w.pair + u) * tt, g, b);
+                            tma_load_5d(sQ + u * kTTile + kTHalf, &qmap, &sm->q_full, 64, 0, (2 * w.pair + u) * tt, g, b);
+                        }
+                    }
+                    ++qc;
+                }
+                if (j == w.nk) break;
+                const int i = kc + j, st = i % kTStages, t = w.t0 + j;
+                const int id_after = j + 2 < w.nk ? page_of(t + 2) : 0;
+                const bool draft = t >= ns;
+                int c1 = draft ? (t - ns) * kTT : t * kTT + x * box_rows, c2 = g, c3 = b;
+                if (!draft && a.c.page) {
+                    if (id < 0 || id >= a.c.n_pages) { tree_flag(a, LVLM_DEV_BOUNDS); id = a.c.n_pages; }    // the copy fills zeros there
+                    c1 &= a.c.page - 1; c2 = id; c3 = 0;
+                }
+                const bool mine = x < (draft ? 1 : boxes);
+                const uint32_t to = st * kTTile + half * kTHalf + (draft ? 0 : x * box_rows * 128);
+                ok = i < kTStages || __all_sync(0xFFFFFFFFu, tree_wait(&sm->k_empty[st], ((i / kTStages) - 1) & 1, sm, a));
+                if (!ok) break;
+                if (lane == 0) mbar_arrive_expect_tx(&sm->k_full[st], kTTile);
+                __syncwarp();
+                if (mine) tma_load_4d(sK + to, draft ? &kdmap : &kmap, &sm->k_full[st], half * 64, c1, c2, c3);
+                ok = i < kTStages || __all_sync(0xFFFFFFFFu, tree_wait(&sm->v_empty[st], ((i / kTStages) - 1) & 1, sm, a));
+                if (!ok) break;
+                if (lane == 0) mbar_arrive_expect_tx(&sm->v_full[st], kTTile);
+                __syncwarp();
+                if (mine) tma_load_4d(sV + to, draft ? &vdmap : &vmap, &sm->v_full[st], half * 64, c1, c2, c3);
+                id = id_next;
+                id_next = id_after;
             }
-            const bool mine = x < (draft ? 1 : boxes);
-            const uint32_t to = st * kTTile + half * kTHalf + (draft ? 0 : x * box_rows * 128);
-            if (j >= kTStages && !__all_sync(0xFFFFFFFFu, tree_wait(&sm->k_empty[st], ((j / kTStages) - 1) & 1, sm, a))) break;
-            if (lane == 0) mbar_arrive_expect_tx(&sm->k_full[st], kTTile);
-            __syncwarp();
-            if (mine) tma_load_4d(sK + to, draft ? &kdmap : &kmap, &sm->k_full[st], half * 64, c1, c2, c3);
-            if (j >= kTStages && !__all_sync(0xFFFFFFFFu, tree_wait(&sm->v_empty[st], ((j / kTStages) - 1) & 1, sm, a))) break;
-            if (lane == 0) mbar_arrive_expect_tx(&sm->v_full[st], kTTile);
-            __syncwarp();
-            if (mine) tma_load_4d(sV + to, draft ? &vdmap : &vmap, &sm->v_full[st], half * 64, c1, c2, c3);
-            id = id_next;
+            kc += w.nk;
         }
-    } else if (warp == 1 && nk > 0) {
+    } else if (warp == 1) {
         // ================= MMA issuer (the whole warp runs the loop, one elected lane issues) =================
         constexpr uint32_t idesc_qk = idesc_bf16_f32(kTT, kTT);
         constexpr uint32_t idesc_pv = idesc_bf16_f32(kTT, kTT) | (1u << 16);     // B (the V tile) is MN-major
         const uint64_t qd0 = smem_desc_sw128(smem_u32(sQ)), kd0 = smem_desc_sw128(smem_u32(sK));
         const uint64_t vd0 = smem_desc_mn_sw128(smem_u32(sV), kTHalf);
-        auto issue_qk = [&](int u, int i) -> bool {
-            const int j = split ? 2 * i + u : i, st = j % kTStages;
-            if (!__all_sync(0xFFFFFFFFu, tree_wait(&sm->k_full[st], (j / kTStages) & 1, sm, a))) return false;
-            tc_fence_after();
-            const uint64_t qd = qd0 + (uint32_t)((split ? 0 : u) * (kTTile >> 4)), kd = kd0 + (uint32_t)(st * (kTTile >> 4));
-            if (elect_one()) {
+        int kc = 0, qc = 0, pc0 = 0, pc1 = 0;                     // of the segments before: key tiles, query tiles, tiles of either half
+        bool ok = true;
+#pragma unroll 1
+        for (int s = 0; ok; ++s) {
+            const TreeSeg w = segment(s);
+            if (w.hd < 0) break;
+            if (w.nk == 0) continue;
+            const int split = w.split, ns = w.ln > 0 ? (w.ln + kTT - 1) / kTT : 0;
+            auto tiles_of = [&](int u) { return split ? (w.nk + 1 - u) / 2 : w.nk; };          // of half u
+            auto issue_qk = [&](int u, int i) -> bool {
+                const int j = kc + (split ? 2 * i + u : i), st = j % kTStages;
+                if (!__all_sync(0xFFFFFFFFu, tree_wait(&sm->k_full[st], (j / kTStages) & 1, sm, a))) return false;
+                tc_fence_after();
+                const uint64_t qd = qd0 + (uint32_t)((split ? 0 : u) * (kTTile >> 4)), kd = kd0 + (uint32_t)(st * (kTTile >> 4));
+                if (elect_one()) {
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    const uint32_t off = ((k >> 2) * kTHalf + (k & 3) * 32) >> 4;
-                    mma_bf16_ss(tmem_base + u * kTT, qd + off, kd + off, idesc_qk, k > 0 ? 1u : 0u);
+                    for (int k = 0; k < 8; ++k) {
+                        const uint32_t off = ((k >> 2) * kTHalf + (k & 3) * 32) >> 4;
+                        mma_bf16_ss(tmem_base + u * kTT, qd + off, kd + off, idesc_qk, k > 0 ? 1u : 0u);
+                    }
+                    mma_commit(&sm->s_full[u]);
+                    if (split || u == 1) mma_commit(&sm->k_empty[st]);
                 }
-                mma_commit(&sm->s_full[u]);
-                if (split || u == 1) mma_commit(&sm->k_empty[st]);
-            }
-            __syncwarp();
-            return true;
-        };
-        bool ok = __all_sync(0xFFFFFFFFu, tree_wait(&sm->q_full, 0, sm, a));
-        for (int u = 0; u < 2; ++u)
-            if (ok && nk2[u] > 0) ok = issue_qk(u, 0);
-        for (int i = 0; ok && i < nk2[0]; ++i) {
-            for (int u = 0; ok && u < 2; ++u) {
-                if (i >= nk2[u]) continue;
-                const int j = split ? 2 * i + u : i, st = j % kTStages, t = t_lo + j;
-                const uint64_t vd = vd0 + (uint32_t)(st * (kTTile >> 4));
-                const uint32_t p_tmem = tmem_base + u * kTT, o_tmem = tmem_base + (2 + u) * kTT;
-                ok = __all_sync(0xFFFFFFFFu, tree_wait(&sm->v_full[st], (j / kTStages) & 1, sm, a));
-                if (!ok) break;
-                if (split || u == 0) {
-                    // rows of the tile that hold keys, rows that hold anything (drafts: the copy has zeroed those from T on)
-                    const int r_lo = t < ns ? ln - t * kTT : n - (t - ns) * kTT, r_hi = t < ns ? kTT : min(kTT, T - (t - ns) * kTT);
-                    if (r_lo < r_hi) {
-                        for (int e = lane; e < (r_hi - r_lo) * 16; e += 32)         // (whole rows: their swizzle does not matter)
-                            *reinterpret_cast<uint4*>(sV + st * kTTile + ((e >> 3) & 1) * kTHalf + (r_lo + (e >> 4)) * 128 + (e & 7) * 16) =
-                                make_uint4(0u, 0u, 0u, 0u);
-                        fence_proxy_async();
+                __syncwarp();
+                return true;
+            };
+            // (the queries come once the epilogue before has read its output, so O may be written as well)
+            ok = __all_sync(0xFFFFFFFFu, tree_wait(&sm->q_full, qc & 1, sm, a));
+#pragma unroll 1
+            for (int u = 0; u < 2; ++u)
+                if (ok && tiles_of(u) > 0) ok = issue_qk(u, 0);
+#pragma unroll 1
+            for (int i = 0; ok && i < tiles_of(0); ++i) {
+#pragma unroll 1
+                for (int u = 0; ok && u < 2; ++u) {
+                    if (i >= tiles_of(u)) continue;
+                    const int jl = split ? 2 * i + u : i, j = kc + jl, st = j % kTStages, t = w.t0 + jl;
+                    const uint64_t vd = vd0 + (uint32_t)(st * (kTTile >> 4));
+                    const uint32_t p_tmem = tmem_base + u * kTT, o_tmem = tmem_base + (2 + u) * kTT;
+                    ok = __all_sync(0xFFFFFFFFu, tree_wait(&sm->v_full[st], (j / kTStages) & 1, sm, a));
+                    if (!ok) break;
+                    if (split || u == 0) {
+                        // rows of the tile that hold keys, rows that hold anything (drafts: the copy has zeroed those from T on)
+                        const int r_lo = t < ns ? w.ln - t * kTT : w.n - (t - ns) * kTT, r_hi = t < ns ? kTT : min(kTT, T - (t - ns) * kTT);
+                        if (r_lo < r_hi) {
+#pragma unroll 1
+                            for (int e = lane; e < (r_hi - r_lo) * 16; e += 32)         // (whole rows: their swizzle does not matter)
+                                *reinterpret_cast<uint4*>(sV + st * kTTile + ((e >> 3) & 1) * kTHalf + (r_lo + (e >> 4)) * 128 + (e & 7) * 16) =
+                                    make_uint4(0u, 0u, 0u, 0u);
+                            fence_proxy_async();
+                            __syncwarp();
+                        }
+                    }
+#pragma unroll
+                    for (int h2 = 0; h2 < 2; ++h2) {
+                        ok = __all_sync(0xFFFFFFFFu, ok && tree_wait(&sm->p_ready[u][h2], ((u ? pc1 : pc0) + i) & 1, sm, a));
+                        if (!ok) break;
+                        tc_fence_after();
+                        if (elect_one()) {
+#pragma unroll
+                            for (int k = h2 * 4; k < h2 * 4 + 4; ++k) {       // 16 keys: heads in 8 columns, remainders 16 columns on
+                                const uint32_t pa = p_tmem + (k >> 1) * 32 + (k & 1) * 8;
+                                mma_bf16_ts(o_tmem, pa, vd + (uint32_t)(k * (2048 >> 4)), idesc_pv, i > 0 || k > 0 ? 1u : 0u);
+                                mma_bf16_ts(o_tmem, pa + 16, vd + (uint32_t)(k * (2048 >> 4)), idesc_pv, 1u);
+                            }
+                            if (h2 == 1) {
+                                if (split || u == 1) mma_commit(&sm->v_empty[st]);
+                                if (i + 1 == tiles_of(u)) mma_commit(&sm->o_done[u]);
+                            }
+                        }
                         __syncwarp();
                     }
+                    if (ok && i + 1 < tiles_of(u)) ok = issue_qk(u, i + 1);
                 }
-#pragma unroll
-                for (int h2 = 0; h2 < 2; ++h2) {
-                    ok = __all_sync(0xFFFFFFFFu, ok && tree_wait(&sm->p_ready[u][h2], i & 1, sm, a));
-                    if (!ok) break;
-                    tc_fence_after();
-                    if (elect_one()) {
-#pragma unroll
-                        for (int k = h2 * 4; k < h2 * 4 + 4; ++k) {       // 16 keys: heads in 8 columns, remainders 16 columns on
-                            const uint32_t pa = p_tmem + (k >> 1) * 32 + (k & 1) * 8;
-                            mma_bf16_ts(o_tmem, pa, vd + (uint32_t)(k * (2048 >> 4)), idesc_pv, i > 0 || k > 0 ? 1u : 0u);
-                            mma_bf16_ts(o_tmem, pa + 16, vd + (uint32_t)(k * (2048 >> 4)), idesc_pv, 1u);
-                        }
-                        if (h2 == 1) {
-                            if (split || u == 1) mma_commit(&sm->v_empty[st]);
-                            if (i + 1 == nk2[u]) mma_commit(&sm->o_done[u]);
-                        }
-                    }
-                    __syncwarp();
-                }
-                if (ok && i + 1 < nk2[u]) ok = issue_qk(u, i + 1);
             }
+            kc += w.nk; ++qc;
+            pc0 += tiles_of(0); pc1 += tiles_of(1);
+        }
+    } else if (warp == 2) {
+        // ================= scheduler: cuts my run into segments =================
+        long long at = lo, p = lo < hi ? sm->first_prefix : 0;    // how far I am; where head hd begins
+        int hd = lo < hi ? sm->first_head : 0, s = 0;
+        TreeHead h = sm->first;
+        bool ok = true, first = true;
+        const int pairs = (a.row_tiles + 1) / 2;
+        while (ok) {
+            TreeSeg w;
+            w.hd = -1;
+            if (at < hi) {
+                const int nt = max(h.nt, 1), x = (int)(at - p);
+                if (x >= nt * h.rt) {
+                    p += nt * h.rt;
+                    h = tree_head(a, ++hd, tt);
+                    continue;
+                }
+                const int fp = h.rt / 2, pair = h.rt <= 2 ? 0 : min((int)((uint32_t)x / (uint32_t)(2 * nt)), fp), wt = pair < fp ? 2 : 1;
+                const long long u0 = p + pair * 2 * nt;           // where the unit begins; a tile weighs wt
+                const int t0 = ((int)(at - u0) + wt - 1) >> (wt - 1), left = (int)min((long long)(wt * nt), hi - u0), t1 = (left + wt - 1) >> (wt - 1);
+                at = u0 + wt * nt;
+                if (t0 >= t1) continue;
+                w.hd = hd; w.pair = pair; w.t0 = t0; w.nk = h.nt > 0 ? t1 - t0 : 0; w.split = wt == 1; w.n = h.n; w.ln = h.ln;
+                w.slot = t0 == 0 && t1 == nt ? -1 : 2 * me + (first ? 0 : 1);
+                first = false;
+                if (t0 == 0 && lane == 0) {
+                    // where the parts of this unit lie: mine, then the first slots of the CTAs up to the one with its last tile
+                    const long long z = u0 + wt * (nt - 1);
+                    a.part_of[(int64_t)hd * pairs + pair] = make_int2(w.slot, z < hi ? 0 : (int)((uint32_t)(z - lo) / (uint32_t)per));
+                }
+            }
+            ok = s < kTSegs || __all_sync(0xFFFFFFFFu, tree_wait(&sm->seg_empty[s % kTSegs], ((s / kTSegs) - 1) & 1, sm, a));
+            if (!ok) break;
+            if (lane == 0) {
+                sm->seg[s % kTSegs] = w;
+                mbar_arrive(&sm->seg_full[s % kTSegs]);
+            }
+            ++s;
+            if (w.hd < 0) break;
         }
     }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kTRegsMany));
         // ================= softmax: thread = query row =================
-        const int u = (warp - 4) >> 2, quarter = warp & 3;
-        const int row = quarter * 32 + lane, tile = 2 * pair + (split ? 0 : u);
+        const int u = (warp - 4) >> 2, quarter = warp & 3, row = quarter * 32 + lane;
+        const uint32_t s_addr = tmem_base + ((uint32_t)(quarter * 32) << 16) + u * kTT, o_addr = s_addr + 2 * kTT;
+        const f32x2 sc = both(a.scale_log2);
+        int jc = 0, oc = 0, xc = 0;                              // of the segments before, or their parity: tiles of my half, outputs of half u (bit u), exchanges
+#pragma unroll 1
+        for (int s = 0;; ++s) {
+        const TreeSeg w = segment(s);
+        if (w.hd < 0) break;
+        const int split = w.split, n = w.n, tile = 2 * w.pair + (split ? 0 : u), b = w.hd / Hkv, g = w.hd % Hkv;
         const int t = tile * tt + row / G;                       // my draft
         const bool mine = row < tt * G && t < n;
         const bool work = __any_sync(0xFFFFFFFFu, mine);         // a warp without rows only keeps the barriers going
-        const uint32_t s_addr = tmem_base + ((uint32_t)(quarter * 32) << 16) + u * kTT, o_addr = s_addr + 2 * kTT;
-        const int n_mine = nk2[u];
-        const f32x2 sc = both(a.scale_log2);
+        const int n_mine = split ? (w.nk + 1 - u) / 2 : w.nk, n_other = split ? (w.nk + u) / 2 : w.nk;
+        const int ns = w.ln > 0 ? (w.ln + kTT - 1) / kTT : 0;
         float m_used = -INFINITY;
         f32x2 l_run = both(0.f);
         bool ok = true;
+#pragma unroll 1
         for (int j = 0; j < n_mine; ++j) {
-            ok = __all_sync(0xFFFFFFFFu, tree_wait(&sm->s_full[u], j & 1, sm, a));
+            ok = __all_sync(0xFFFFFFFFu, tree_wait(&sm->s_full[u], (jc + j) & 1, sm, a));
             if (!ok) break;
             tc_fence_after();
             if (!work) {
@@ -230,20 +387,14 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
 #pragma unroll
             for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + c * 32, v[c]);
             tmem_ld_wait();
-            const int kt = t_lo + (split ? 2 * j + u : j);       // my key tile
-            if (kt < ns) {
-                const int lim = ln - kt * kTT;                   // the same for all rows
-                if (lim < kTT) {
-#pragma unroll
-                    for (int c = 0; c < 4; ++c)
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) v[c][e] = c * 32 + e < lim ? v[c][e] : -INFINITY;
-                }
-            } else {
-                const int w0 = (kt - ns) * (kTT / 32);
+            const int kt = w.t0 + (split ? 2 * j + u : j);       // my key tile
+            const int lim = kt < ns ? w.ln - kt * kTT : 0;       // a tile of the cache: rows that hold keys, the same for all
+            if (lim < kTT) {
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
-                    const uint32_t bits = mine ? tree_see(a, b, t, n, w0 + c) : 0u;
+                    uint32_t bits;
+                    if (kt < ns) bits = lim >= c * 32 + 32 ? 0xFFFFFFFFu : lim <= c * 32 ? 0u : (1u << (lim - c * 32)) - 1u;
+                    else bits = mine ? tree_see(a, b, t, n, (kt - ns) * (kTT / 32) + c) : 0u;
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[c][e] = (bits >> e) & 1u ? v[c][e] : -INFINITY;
                 }
@@ -303,77 +454,92 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         float l0, l1;
         unpack2(l_run, l0, l1);
         float l_row = l0 + l1, f0 = 1.f, f1 = 0.f;
+        if (w.nk == 0) {                                         // no key at all: zeros (such a unit is never cut)
+#pragma unroll 1
+            for (int r = 0; r < 32; ++r) {
+                const int rr = quarter * 32 + r, td = tile * tt + rr / G;
+                if ((split && u == 1) || rr >= tt * G || td >= n) continue;
+                *reinterpret_cast<uint2*>(a.out + (((int64_t)b * T + td) * a.H + g * G + rr % G) * kHeadDim + lane * 4) = make_uint2(0u, 0u);
+            }
+            if (mine && a.lse && (!split || u == 0)) a.lse[((int64_t)b * a.H + g * G + row % G) * T + t] = -INFINITY;
+            continue;
+        }
         if (split) {
             sm->xm[u][row] = m_used;
             sm->xl[u][row] = l_row;
-            asm volatile("bar.sync 1, %0;" ::"n"(2 * kTT) : "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sm->x_ready);
+            ok = ok && tree_wait(&sm->x_ready, xc, sm, a);
+            xc ^= 1;
             const float m0 = sm->xm[0][row], m1 = sm->xm[1][row];
             m_used = fmaxf(m0, m1);
             f0 = m0 > -INFINITY ? ex2_fast(m0 - m_used) : 0.f;
             f1 = m1 > -INFINITY ? ex2_fast(m1 - m_used) : 0.f;
             l_row = sm->xl[0][row] * f0 + sm->xl[1][row] * f1;
-            for (int x = 0; x < 2; ++x) ok = ok && (nk2[x] == 0 || tree_wait(&sm->o_done[x], 0, sm, a));
-        } else if (n_mine > 0) {
-            ok = ok && tree_wait(&sm->o_done[u], 0, sm, a);
+            ok = ok && (n_mine == 0 || tree_wait(&sm->o_done[u], (oc >> u) & 1, sm, a));
+            ok = ok && (n_other == 0 || tree_wait(&sm->o_done[u ^ 1], (oc >> (u ^ 1)) & 1, sm, a));
+        } else {
+            ok = ok && tree_wait(&sm->o_done[u], (oc >> u) & 1, sm, a);
         }
         ok = __all_sync(0xFFFFFFFFu, ok) && !sm->abort;
         tc_fence_after();
         if (ok && work) {
-            const bool last = a.S == 1;
-            const float inv = last ? (l_row > 0.f ? 1.0f / l_row : 0.f) : 1.f;
             const uint32_t oa = split ? o_addr - u * kTT : o_addr;       // O of half 0, or of my tile
-            const int64_t slot = (((int64_t)hd * a.row_tiles + tile) * a.S + part) * kTT;
-            unsigned char* stage = sQ + (warp - 4) * 8192;
-            const int rowB = last ? 128 : 256, msk = rowB / 16 - 1;
+            const int c_lo = split ? 64 * u : 0, c_hi = split ? c_lo + 64 : kTT;     // one row tile: a half finishes half of the channels
+            const int place = split ? row : u * kTT + row;
+            const float inv = w.slot >= 0 ? 1.f : l_row > 0.f ? 1.0f / l_row : 0.f;
+            f0 *= inv; f1 *= inv;
+            const int my_at = mine ? t * a.H + row % G : -1;             // my row of the sequence's output
+            __nv_bfloat16* out = a.out + ((int64_t)b * T * a.H + g * G) * kHeadDim + (lane & 3) * 8;
+            float4* part = reinterpret_cast<float4*>(a.part_o + (int64_t)w.slot * a.pitch * kHeadDim) + place;
+            unsigned char* stage = sQ + (warp - 4) * 2048;
 #pragma unroll 1
-            for (int ch0 = split ? 64 * u : 0; ch0 < (split ? 64 * u + 64 : kTT); ch0 += 64) {
-#pragma unroll 1
-                for (int c = 0; c < 2; ++c) {
-                    float o[32];
-                    if (nk > 0) {
-                        tmem_ld32(oa + ch0 + c * 32, o);
-                        tmem_ld_wait();
-                    }
+            for (int c0 = c_lo; c0 < c_hi; c0 += 32) {                   // 32 channels at a time
+                float o[32];
+                tmem_ld32(oa + c0, o);
+                tmem_ld_wait();
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) o[e] = nk > 0 && f0 > 0.f ? o[e] * f0 : 0.f;
-                    if (split && nk2[1] > 0) {
-                        float p[32];
-                        tmem_ld32(oa + kTT + ch0 + c * 32, p);
-                        tmem_ld_wait();
+                for (int e = 0; e < 32; ++e) o[e] = f0 > 0.f ? o[e] * f0 : 0.f;
+                if (split && w.nk > 1) {
+                    float p[32];
+                    tmem_ld32(oa + kTT + c0, p);
+                    tmem_ld_wait();
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) o[e] = f1 > 0.f ? fmaf(p[e], f1, o[e]) : o[e];
-                    }
-                    if (last) {
-#pragma unroll
-                        for (int q = 0; q < 4; ++q)
-                            *reinterpret_cast<uint4*>(stage + lane * rowB + (((4 * c + q) ^ (lane & msk)) << 4)) =
-                                make_uint4(pack_bf16(o[8 * q] * inv, o[8 * q + 1] * inv), pack_bf16(o[8 * q + 2] * inv, o[8 * q + 3] * inv),
-                                           pack_bf16(o[8 * q + 4] * inv, o[8 * q + 5] * inv), pack_bf16(o[8 * q + 6] * inv, o[8 * q + 7] * inv));
-                    } else {
-#pragma unroll
-                        for (int q = 0; q < 8; ++q)
-                            *reinterpret_cast<float4*>(stage + lane * rowB + (((8 * c + q) ^ (lane & msk)) << 4)) =
-                                make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
-                    }
+                    for (int e = 0; e < 32; ++e) o[e] = f1 > 0.f ? fmaf(p[e], f1, o[e]) : o[e];
                 }
-                __syncwarp();
-                const int step = 512 / rowB, ch = lane & msk;
-#pragma unroll 4
-                for (int r = lane / (rowB / 16); r < 32; r += step) {
-                    const uint4 x = *reinterpret_cast<const uint4*>(stage + r * rowB + ((ch ^ (r & msk)) << 4));
-                    const int rr = quarter * 32 + r, td = tile * tt + rr / G;
-                    if (rr >= tt * G || td >= n) continue;
-                    if (last)
-                        *reinterpret_cast<uint4*>(a.out + (((int64_t)b * T + td) * a.H + g * G + rr % G) * kHeadDim + ch0 + ch * 8) = x;
-                    else
-                        *reinterpret_cast<uint4*>(a.part_o + (slot + rr) * kHeadDim + ch0 + ch * 4) = x;
+                if (w.slot >= 0) {
+                    // a part: groups of four channels of all rows side by side, so that the threads' stores are
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) part[(c0 / 4 + q) * a.pitch] = make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
+                } else {
+                    // the rows themselves, through shared memory (the Q tile, which nobody needs any more)
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        *reinterpret_cast<uint4*>(stage + lane * 64 + ((q ^ (lane >> 1 & 3)) << 4)) =
+                            make_uint4(pack_bf16(o[8 * q], o[8 * q + 1]), pack_bf16(o[8 * q + 2], o[8 * q + 3]),
+                                       pack_bf16(o[8 * q + 4], o[8 * q + 5]), pack_bf16(o[8 * q + 6], o[8 * q + 7]));
+                    __syncwarp();
+#pragma unroll
+                    for (int r0 = 0; r0 < 32; r0 += 8) {
+                        const int r = r0 + (lane >> 2), at = __shfl_sync(0xFFFFFFFFu, my_at, r);
+                        const uint4 x = *reinterpret_cast<const uint4*>(stage + r * 64 + (((lane & 3) ^ (r >> 1 & 3)) << 4));
+                        if (at >= 0) *reinterpret_cast<uint4*>(out + (int64_t)at * kHeadDim + c0) = x;
+                    }
+                    __syncwarp();
                 }
-                __syncwarp();
             }
-            if (mine && (!split || u == 0)) {
-                if (!last) a.part_ml[slot + row] = make_float2(m_used, l_row);
-                else if (a.lse) a.lse[((int64_t)b * a.H + g * G + row % G) * T + t] = l_row > 0.f ? (m_used + log2f(l_row)) * kTreeLn2 : -INFINITY;
+            if (!split || u == 0) {
+                if (w.slot >= 0) a.part_ml[(int64_t)w.slot * a.pitch + place] = make_float2(m_used, l_row);
+                else if (mine && a.lse) a.lse[((int64_t)b * a.H + g * G + row % G) * T + t] = l_row > 0.f ? (m_used + log2f(l_row)) * kTreeLn2 : -INFINITY;
             }
+        }
+        oc ^= split && w.nk == 1 ? 1 : 3;
+        jc += n_mine;
+        // the next queries may come, the next output may be written
+        fence_proxy_async();
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&sm->e_done);
         }
     }
     tc_fence_before();
@@ -396,9 +562,7 @@ lvlm_status launch_tree_tc(const TreeArgs& a, const TreeMaps& m, cudaStream_t st
         return cudaFuncGetAttributes(&f, tree_tc_kernel) == cudaSuccess ? f.numRegs : 0;
     }();
     if (3 * regs < kTRegsFew + 2 * kTRegsMany) return LVLM_ERR_CUDA;       // the split would wait for registers that nobody has
-    const int64_t ctas = (int64_t)a.B * a.c.Hkv * a.S * ((a.row_tiles + 1) / 2);
-    if (ctas > 0x7FFFFFFFll) return LVLM_ERR_UNSUPPORTED;
-    return launch_kernel(tree_tc_kernel, dim3((unsigned)ctas), dim3(kTThreads), smem, stream, 1, m.q, m.k, m.v, m.kd, m.vd, a);
+    return launch_kernel(tree_tc_kernel, dim3((unsigned)a.S), dim3(kTThreads), smem, stream, 1, m.q, m.k, m.v, m.kd, m.vd, a);
 }
 
 }  // namespace lvlm

@@ -340,6 +340,19 @@ def test_tree_attn_wide(B, H, Hkv, T, lens, count, kind, page):
     run_tree(B, H, Hkv, T, lens, count, page, kind, seed=T)
 
 
+@pytest.mark.parametrize("B,H,Hkv,T,page,seed", [
+    (5, 32, 8, 13, 64, 1), (60, 32, 8, 5, 16, 2), (9, 28, 4, 40, 0, 3), (2, 48, 8, 44, 128, 4), (130, 12, 4, 7, 0, 5), (1, 6, 1, 150, 32, 6)])
+def test_tree_attn_ragged_over_the_gpu(B, H, Hkv, T, page, seed):
+    """Ragged lengths and counts, nothing at all among them: the run of a CTA begins and ends anywhere."""
+    r = np.random.default_rng(seed)
+    lens = r.integers(0, 700 if B < 20 else 150, size=(B, Hkv))
+    lens[r.random((B, Hkv)) < 0.15] = 0
+    lens.reshape(-1)[:3] = ([1500, 0, 128] if B < 20 else [300, 0, 128])[:lens.size]
+    count = np.where(r.random(B) < 0.2, 0, r.integers(1, T + 1, size=B))
+    count[0] = T
+    run_tree(B, H, Hkv, T, lens.reshape(-1).tolist(), count.tolist(), page, "any", seed=seed)
+
+
 @pytest.mark.parametrize("max_len", [None, 1, 100, 3001, 100000])
 @pytest.mark.parametrize("T,page", [(1, 0), (3, 64), (20, 16)])
 def test_tree_attn_split_however(max_len, T, page):
