@@ -4,11 +4,11 @@
 // For every (sequence, KV head) the T G query rows of the group (row r = draft r / G, head r % G of the group) meet the
 // same keys: len cache rows, then the count drafts.  An online softmax runs over the keys.
 //
-// Few rows (tree_mma_kernel, here): a tile of 16 query rows on mma.sync.  The keys of a head are cut into runs for the CTAs of a
-// cluster.  A CTA is a producer warp and four compute warps around a ring of stages of 64 keys, fetched by TMA tile copies (a box per
-// page and 64 channels); a compute warp takes 16 keys of a stage.  The warps are added in shared memory, the CTAs of the cluster
-// through distributed shared memory: one launch, no workspace.
-// Many rows or keys: tree_tc.cu, on tcgen05; parts of a unit that it cut are added by tree_combine_kernel, here.
+// Few rows (tree_mma_kernel, here): mma.sync, one or two groups of 16 query rows a CTA.  A CTA is a producer warp and four compute
+// warps a group around a ring of stages of 64 keys, fetched by TMA tile copies (a box per page and 64 channels); a warp takes 16
+// keys of a stage.  The keys of a head are cut into runs for the CTAs of a cluster; the warps are added in shared memory, the CTAs through
+// distributed shared memory: one launch, no workspace.
+// Many rows, or few heads with many keys: tree_tc.cu, on tcgen05; parts of a unit that it cut are added by tree_combine_kernel, here.
 #include "exp2.cuh"
 #include "sm100.cuh"
 #include "tree_attn.cuh"
@@ -17,19 +17,20 @@ namespace lvlm {
 
 using namespace sm100;
 
-constexpr int kTreeWarps = 4;
-constexpr int kTreeThreads = (kTreeWarps + 1) * 32;
-constexpr int kTreeRows = 16;                        // query rows a CTA
+constexpr int kTreeRows = 16;                        // query rows of a group
 constexpr int kTreeStageKeys = 64;
 constexpr int kTreeBox = kTreeStageKeys * 128;       // 64 keys x 64 channels
 constexpr int kTreeStageBytes = 4 * kTreeBox;        // K low, K high, V low, V high channels
-constexpr int kTreeStages = 3;
-constexpr int kTreeTargetCtas = 2 * 148;             // CTAs wanted in flight, two an SM
 constexpr int kTreeMaxCluster = 8;
 constexpr int kTreeMmaWords = 2;                     // mask words of a row: T <= 64
+constexpr int kTreePitch = kHeadDim + 4;             // of a row of the results in shared memory
 
-// Which kernel.
-static bool tree_uses_tc(int T, int64_t rows, int64_t) { return rows > kTreeRows || T > 32 * kTreeMmaWords; }
+// R groups: two CTAs an SM with a ring of 96 KB each, or one with 192 KB.
+template <int R> struct TreeMma {
+    static constexpr int kWarps = 4 * R, kThreads = (kWarps + 1) * 32, kStages = R == 1 ? 3 : 6;
+    static constexpr size_t kSmem = 1024 + (size_t)kStages * kTreeStageBytes;
+    static_assert(kSmem <= kMaxDynSmem && kWarps * kTreeRows * kTreePitch * 4 <= kStages * kTreeStageBytes, "");
+};
 
 __device__ __forceinline__ void tree_ldmatrix(uint32_t addr, uint32_t* r) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];\n"
@@ -53,35 +54,35 @@ __device__ __forceinline__ uint32_t tree_off(int r, int ch) {
     return (uint32_t)((ch >> 3) * kTreeBox + r * 128 + (((ch & 7) ^ (r & 7)) << 4));
 }
 
-// grid.x = heads * row_tiles * S, clusters of S CTAs
-__global__ void __launch_bounds__(kTreeThreads, 2)
+// grid.x = (head, rank), clusters of S CTAs: all rows of a head are a CTA's
+template <int R>
+__global__ void __launch_bounds__(TreeMma<R>::kThreads, R == 1 ? 2 : 1)
 tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
                 const __grid_constant__ CUtensorMap kdmap, const __grid_constant__ CUtensorMap vdmap, const TreeArgs a) {
+    constexpr int kWarps = TreeMma<R>::kWarps, kThreads = TreeMma<R>::kThreads, kStages = TreeMma<R>::kStages, kRows = R * kTreeRows;
     extern __shared__ __align__(1024) unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    __shared__ uint64_t s_full[kTreeStages], s_empty[kTreeStages];
-    __shared__ float2 s_ml[kTreeWarps][kTreeRows], s_ML[kTreeRows];
+    __shared__ uint64_t s_full[kStages], s_empty[kStages];
+    __shared__ float2 s_ml[kWarps][kTreeRows], s_ML[kRows];
     __shared__ int s_abort;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     if (tid == 0) {
-        for (int s = 0; s < kTreeStages; ++s) { mbar_init(&s_full[s], 1); mbar_init(&s_empty[s], kTreeWarps); }
+        for (int s = 0; s < kStages; ++s) { mbar_init(&s_full[s], 1); mbar_init(&s_empty[s], kWarps); }
         s_abort = 0;
         fence_barrier_init();
     }
+    if (tid == 32) { prefetch_tmap(&kmap); prefetch_tmap(&vmap); prefetch_tmap(&kdmap); prefetch_tmap(&vdmap); }
     __syncthreads();
     pdl_enter();
     const int S = a.S, T = a.T, G = a.G, Hkv = a.c.Hkv;
-    const int part = (int)cluster_ctarank(), tile = blockIdx.x / S % a.row_tiles, hd = blockIdx.x / S / a.row_tiles;
-    const int b = hd / Hkv, g = hd % Hkv, r0 = tile * kTreeRows;
-    const int n = tree_count(a, b), rows = n * G;               // rows behind `rows` are not asked for
-    if (r0 >= rows) return;
-    const int ln = tree_len(a, hd);
-    // stages of the cache, then of the drafts; a head whose length is bad has none and gives zeros
-    const int ns = ln > 0 ? (ln + kTreeStageKeys - 1) / kTreeStageKeys : 0;
-    const int nt = ln < 0 ? 0 : ns + (a.drafts ? (n + kTreeStageKeys - 1) / kTreeStageKeys : 0);
-    const int per = (nt + S - 1) / S, t_lo = min(nt, part * per), nstage = min(nt, t_lo + per) - t_lo;
+    const int part = (int)cluster_ctarank(), hd = blockIdx.x / S, b = hd / Hkv, g = hd % Hkv;
+    const TreeHead h = tree_head(a, hd, kTreeStageKeys);
+    const int n = h.n, ln = h.ln, ns = h.ns, rows = n * G;      // rows behind `rows` are not asked for
+    if (rows == 0) return;
+    // a head whose length is bad has no keys and gives zeros
+    const int per = (h.nt + S - 1) / S, t_lo = min(h.nt, part * per), nstage = min(h.nt, t_lo + per) - t_lo;
 
-    const int row = lane >> 2, qd = lane & 3;                   // my rows row and row + 8 of the tile
+    const int row = lane >> 2, qd = lane & 3, kq = warp & 3, gr0 = (warp >> 2) * kTreeRows;          // my group's rows; mine are row and row + 8 of them
     float o[16][4], m_run[2] = {-INFINITY, -INFINITY}, l_run[2] = {0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 16; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
@@ -93,7 +94,7 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         tree_flag(a, LVLM_DEV_TIMEOUT);
         return false;
     };
-    if (warp == kTreeWarps) {
+    if (warp == kWarps) {
         // ---- producer: lane i copies the i-th box of K and V halves of a stage ----------------------------------
         const int box_rows = a.c.page ? min(a.c.page, kTreeStageKeys) : kTreeStageKeys, boxes = kTreeStageKeys / box_rows;    // 1, 2 or 4
         const int quarter = lane & 3, bx = lane >> 2;
@@ -104,9 +105,9 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         };
         int id = page_of(t_lo);
         for (int i = 0; i < nstage; ++i) {
-            const int s = i % kTreeStages, st = t_lo + i;
+            const int s = i % kStages, st = t_lo + i;
             const int id_next = i + 1 < nstage ? page_of(st + 1) : 0;      // asked for a stage ahead
-            if (i >= kTreeStages && !__all_sync(0xFFFFFFFFu, wait_on(&s_empty[s], (uint32_t)(i / kTreeStages - 1) & 1u))) break;
+            if (i >= kStages && !__all_sync(0xFFFFFFFFu, wait_on(&s_empty[s], (uint32_t)(i / kStages - 1) & 1u))) break;
             if (lane == 0) mbar_arrive_expect_tx(&s_full[s], kTreeStageBytes);
             __syncwarp();
             unsigned char* to = smem + s * kTreeStageBytes + quarter * kTreeBox;
@@ -128,7 +129,7 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         uint32_t see[2][kTreeMmaWords];                         // draft mask of my two rows
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            const int r = r0 + row + 8 * u, t = r / G, hh = r % G;
+            const int r = gr0 + row + 8 * u, t = r / G, hh = r % G;
             qp[u] = r < rows ? reinterpret_cast<const uint32_t*>(a.q + (int64_t)b * a.q_sb + (int64_t)t * a.q_sn + (int64_t)(g * G + hh) * a.q_sh) : nullptr;
 #pragma unroll
             for (int w = 0; w < kTreeMmaWords; ++w) see[u][w] = r < rows ? tree_see(a, b, t, n, w) : 0u;
@@ -141,14 +142,15 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                 qa[ks][2 + u] = qp[u] ? *(qp[u] + ks * 8 + 4 + qd) : 0u;
             }
         for (int i = 0; i < nstage; ++i) {
-            const int s = i % kTreeStages, st = t_lo + i;
+            const int s = i % kStages, st = t_lo + i;
             const bool draft = st >= ns;
-            const int k0 = (draft ? st - ns : st) * kTreeStageKeys + warp * 16, kend = draft ? n : ln;   // my keys, of how many
-            const bool ok = __all_sync(0xFFFFFFFFu, wait_on(&s_full[s], (uint32_t)(i / kTreeStages) & 1u));
-            if (ok && k0 < kend) {
+            const int k0 = (draft ? st - ns : st) * kTreeStageKeys + kq * 16, kend = draft ? n : ln;   // my keys, of how many
+            const bool ok = __all_sync(0xFFFFFFFFu, wait_on(&s_full[s], (uint32_t)(i / kStages) & 1u));
+            if (ok && k0 < kend && gr0 < rows) {
                 const uint32_t at = smem_u32(smem) + s * kTreeStageBytes;
-                const int rr = warp * 16;
-                if (k0 + 16 > kend) {                           // rows behind the end hold anything: their weight is zero, so must be V
+                const int rr = kq * 16;
+                // rows behind the end hold anything: their weight is zero, so must be V (every group's warp writes the zeros that it reads)
+                if (k0 + 16 > kend) {
                     for (int e = lane; e < (k0 + 16 - kend) * 16; e += 32)
                         asm volatile("st.shared.v4.b32 [%0], {%1, %1, %1, %1};"
                                      ::"r"(at + 2 * kTreeBox + tree_off(rr + (kend - k0) + (e >> 4), e & 15)), "r"(0u) : "memory");
@@ -234,9 +236,8 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
         for (int i = 0; i < 1000; ++i) __nanosleep(1000);
         __syncthreads();
     }
-    float* so = reinterpret_cast<float*>(smem);                 // [4][16][132]
-    constexpr int kPitch = kHeadDim + 4;
-    if (warp < kTreeWarps) {
+    float* so = reinterpret_cast<float*>(smem);                 // [warps][16][132]
+    if (warp < kWarps) {
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             l_run[u] += __shfl_xor_sync(0xFFFFFFFFu, l_run[u], 1);
@@ -244,32 +245,35 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             if (qd == 0) s_ml[warp][row + 8 * u] = make_float2(m_run[u], l_run[u]);
 #pragma unroll
             for (int c = 0; c < 16; ++c)
-                *reinterpret_cast<float2*>(so + (warp * kTreeRows + row + 8 * u) * kPitch + c * 8 + qd * 2) = make_float2(o[c][2 * u], o[c][2 * u + 1]);
+                *reinterpret_cast<float2*>(so + (warp * kTreeRows + row + 8 * u) * kTreePitch + c * 8 + qd * 2) = make_float2(o[c][2 * u], o[c][2 * u + 1]);
         }
     }
     __syncthreads();
-    for (int idx = tid; idx < kTreeRows * (kHeadDim / 4); idx += kTreeThreads) {
+    for (int idx = tid; idx < kRows * (kHeadDim / 4); idx += kThreads) {
         const int rr = idx / (kHeadDim / 4), c4 = idx % (kHeadDim / 4);
+        const int w0 = rr / kTreeRows * 4, rg = rr % kTreeRows;
         float M = -INFINITY, Ls = 0.f;
         float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-        for (int w = 0; w < kTreeWarps; ++w) M = fmaxf(M, s_ml[w][rr].x);
+        for (int w = 0; w < 4; ++w) M = fmaxf(M, s_ml[w0 + w][rg].x);
 #pragma unroll
-        for (int w = 0; w < kTreeWarps; ++w) {
-            const float2 ml = s_ml[w][rr];
+        for (int w = 0; w < 4; ++w) {
+            const float2 ml = s_ml[w0 + w][rg];
             const float f = ml.x > -INFINITY ? ex2_fast(ml.x - M) : 0.f;
-            const float4 x = *reinterpret_cast<const float4*>(so + (w * kTreeRows + rr) * kPitch + c4 * 4);
+            const float4 x = *reinterpret_cast<const float4*>(so + ((w0 + w) * kTreeRows + rg) * kTreePitch + c4 * 4);
             v.x += x.x * f; v.y += x.y * f; v.z += x.z * f; v.w += x.w * f;
             Ls += ml.y * f;
         }
-        *reinterpret_cast<float4*>(so + rr * kPitch + c4 * 4) = v;      // (over the first warp's, which only this thread reads)
+        // (over the group's first warp's, which only this thread reads)
+        *reinterpret_cast<float4*>(so + (w0 * kTreeRows + rg) * kTreePitch + c4 * 4) = v;
         if (c4 == 0) s_ML[rr] = make_float2(M, Ls);
     }
     // ---- the CTAs of the cluster, in rank order; a CTA finishes a slice of the rows and channels ---------------------------
     cluster_barrier();
-    for (int idx = part * kTreeThreads + tid; idx < kTreeRows * (kHeadDim / 4); idx += S * kTreeThreads) {
-        const int rr = idx / (kHeadDim / 4), c4 = idx % (kHeadDim / 4), r = r0 + rr;
-        if (r >= rows) continue;
+    for (int idx = part * kThreads + tid; idx < kRows * (kHeadDim / 4); idx += S * kThreads) {
+        const int rr = idx / (kHeadDim / 4), c4 = idx % (kHeadDim / 4);
+        if (rr >= rows) continue;
+        const float* mine = so + (rr / kTreeRows * 4 * kTreeRows + rr % kTreeRows) * kTreePitch + c4 * 4;
         float2 ml[kTreeMaxCluster];
         float4 x[kTreeMaxCluster];
 #pragma unroll
@@ -278,7 +282,7 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             x[c] = make_float4(0.f, 0.f, 0.f, 0.f);
             if (c < S) {
                 ml[c] = cluster_ld(&s_ML[rr], c);
-                x[c] = cluster_ld(reinterpret_cast<const float4*>(so + rr * kPitch + c4 * 4), c);
+                x[c] = cluster_ld(reinterpret_cast<const float4*>(mine), c);
             }
         }
         float M = -INFINITY, Ls = 0.f;
@@ -291,99 +295,154 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             v.x += x[c].x * f; v.y += x[c].y * f; v.z += x[c].z * f; v.w += x[c].w * f;
             Ls += ml[c].y * f;
         }
-        const int t = r / G, h = g * G + r % G;
+        const int t = rr / G, hq = g * G + rr % G;
         const float inv = Ls > 0.f ? 1.0f / Ls : 0.f;
-        *reinterpret_cast<uint2*>(a.out + (((int64_t)b * T + t) * a.H + h) * kHeadDim + c4 * 4) =
+        *reinterpret_cast<uint2*>(a.out + (((int64_t)b * T + t) * a.H + hq) * kHeadDim + c4 * 4) =
             make_uint2(pack_bf16(v.x * inv, v.y * inv), pack_bf16(v.z * inv, v.w * inv));
-        if (a.lse && c4 == 0) a.lse[((int64_t)b * a.H + h) * T + t] = Ls > 0.f ? (M + log2f(Ls)) * kTreeLn2 : -INFINITY;
+        if (a.lse && c4 == 0) a.lse[((int64_t)b * a.H + hq) * T + t] = Ls > 0.f ? (M + log2f(Ls)) * kTreeLn2 : -INFINITY;
     }
     cluster_arrive_exec();                                      // my reads of the other CTAs' shared memory are done
     cluster_wait();                                             // and nobody leaves while its own is still read
 }
 
-// Adds the parts of a unit (a pair of row tiles of a head) that the tcgen05 kernel cut, in order.  Lane = row, a warp CH groups of four
+// Adds the parts of a unit that was cut, in order.  Lane = row, a warp CH groups of four
 // channels of 32 rows: the loads are the lines that the parts were stored in.  grid (units, row blocks, channel blocks).
+// Bound by latency where parts are many: lengths are read before the wait for the kernel ahead (it has waited for whatever wrote
+// them), the first outputs are on their way while the weights are worked out, which the warps share.
 constexpr int kTreeCombineWarps = 8;
+constexpr int kTreeMostParts = kTreeTcCtas;
 template <int CH>
 __global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(const TreeArgs a) {
+    __shared__ float s_m[kTreeMostParts][32], s_l[kTreeMostParts][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int hd = blockIdx.x / a.units, unit = blockIdx.x % a.units, b = hd / a.c.Hkv, g = hd % a.c.Hkv;
+    const int place = blockIdx.y * 32 + lane, row = place % kTreeTcRows, tile = unit * a.unit_tiles + place / kTreeTcRows;
+    const TreeHead h = tree_head(a, hd, kTreeTcRows);
     pdl_enter();
-    const int pairs = (a.row_tiles + 1) / 2, lane = threadIdx.x & 31;
-    const int2 of = a.part_of[blockIdx.x];
-    const int hd = blockIdx.x / pairs, pair = blockIdx.x % pairs, b = hd / a.c.Hkv, g = hd % a.c.Hkv, tt = a.tile_rows / a.G;
-    const int place = blockIdx.y * 32 + lane, row = place % kTreeTcRows, tile = 2 * pair + place / kTreeTcRows;
-    const int n = tree_count(a, b);
-    if (2 * pair * tt >= n || of.x < 0) return;                 // nothing asked for, or not cut (of is only written where something is)
-    const int t = tile * tt + row / a.G;
-    const bool mine = row < a.tile_rows && t < n;
-    const int c0 = (blockIdx.z * kTreeCombineWarps + (threadIdx.x >> 5)) * CH, parts = of.y + 1;
-    // part p >= 1 lies in the first slot of its CTA
-    const int64_t rest = (int64_t)(of.x & ~1);
-    auto slot = [&](int p) -> int64_t { return p == 0 ? of.x : rest + 2 * p; };
-    float M = -INFINITY;
-#pragma unroll 4
-    for (int p = 0; p < parts; ++p) M = fmaxf(M, a.part_ml[slot(p) * a.pitch + place].x);
+    if (unit * a.unit_tiles * a.tile_rows >= h.n * a.G) return; // nothing asked for
+    int2 of;                                                    // first slot and how many more parts
+    int stride;                                                 // slots between the CTAs of a unit's parts
+    if (a.runs) {
+        of = a.part_of[blockIdx.x];
+        stride = 2;
+    } else {
+        const int step = tree_part(h, a.S);
+        of = make_int2(step >= h.nt ? -1 : hd * a.S * a.units + unit, (h.nt - 1) / step);
+        stride = a.units;
+    }
+    if (of.x < 0) return;                                       // not cut
+    const int r = tile * a.tile_rows + row, t = r / a.G;
+    const bool mine = row < a.tile_rows && t < h.n;
+    const int c0 = (blockIdx.z * kTreeCombineWarps + warp) * CH, parts = min(of.y + 1, kTreeMostParts);
+    // (runs: part p >= 1 lies in the first slot of its CTA)
+    const int rest = a.runs ? of.x & ~1 : of.x;
+    auto slot = [&](int p) -> int64_t { return p == 0 ? of.x : rest + stride * p; };
+    constexpr int kAhead = 16 / CH;
+    float4 x[kAhead][CH];
+    auto fetch = [&](int p0) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u)
+            if (p0 + u < parts) {
+                const float4* from = reinterpret_cast<const float4*>(a.part_o + slot(p0 + u) * a.pitch * kHeadDim) + place;
+#pragma unroll
+                for (int c = 0; c < CH; ++c) x[u][c] = from[(c0 + c) * a.pitch];
+            }
+    };
+    fetch(0);
+    for (int p = warp; p < parts; p += kTreeCombineWarps) {
+        const float2 ml = a.part_ml[slot(p) * a.pitch + place];
+        s_m[p][lane] = ml.x;
+        s_l[p][lane] = ml.y;
+    }
+    __syncthreads();
+    float M = -INFINITY, Ls = 0.f;
+    for (int p = 0; p < parts; ++p) M = fmaxf(M, s_m[p][lane]);
     float4 v[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) v[c] = make_float4(0.f, 0.f, 0.f, 0.f);
-    float Ls = 0.f;
-    constexpr int kAhead = 8 / CH;
-    for (int p0 = 0; p0 < parts; p0 += kAhead) {
-        float4 x[kAhead][CH];
-        float2 ml[kAhead];
+    for (int p0 = 0;;) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            ml[u] = make_float2(-INFINITY, 0.f);
-            if (p0 + u < parts) {
-                const int64_t s = slot(p0 + u);
-                ml[u] = a.part_ml[s * a.pitch + place];
-#pragma unroll
-                for (int c = 0; c < CH; ++c) x[u][c] = reinterpret_cast<const float4*>(a.part_o + s * a.pitch * kHeadDim)[(int64_t)(c0 + c) * a.pitch + place];
-            }
-        }
-#pragma unroll
-        for (int u = 0; u < kAhead; ++u) {
-            if (ml[u].x == -INFINITY) continue;
-            const float w = ex2_fast(ml[u].x - M);
-            Ls += ml[u].y * w;
+            if (p0 + u >= parts) break;
+            const float m = s_m[p0 + u][lane];
+            if (m == -INFINITY) continue;                       // (without weight)
+            const float w = ex2_fast(m - M);
+            Ls += s_l[p0 + u][lane] * w;
 #pragma unroll
             for (int c = 0; c < CH; ++c) { v[c].x += x[u][c].x * w; v[c].y += x[u][c].y * w; v[c].z += x[u][c].z * w; v[c].w += x[u][c].w * w; }
         }
+        p0 += kAhead;
+        if (p0 >= parts) break;
+        fetch(p0);
     }
     if (!mine) return;
-    const int h = g * a.G + row % a.G;
+    const int head = g * a.G + r % a.G;
     const float inv = Ls > 0.f ? 1.0f / Ls : 0.f;
-    uint2* to = reinterpret_cast<uint2*>(a.out + (((int64_t)b * a.T + t) * a.H + h) * kHeadDim) + c0;
+    uint2* to = reinterpret_cast<uint2*>(a.out + (((int64_t)b * a.T + t) * a.H + head) * kHeadDim) + c0;
 #pragma unroll
     for (int c = 0; c < CH; ++c) to[c] = make_uint2(pack_bf16(v[c].x * inv, v[c].y * inv), pack_bf16(v[c].z * inv, v[c].w * inv));
-    if (a.lse && c0 == 0) a.lse[((int64_t)b * a.H + h) * a.T + t] = Ls > 0.f ? (M + log2f(Ls)) * kTreeLn2 : -INFINITY;
+    if (a.lse && c0 == 0) a.lse[((int64_t)b * a.H + head) * a.T + t] = Ls > 0.f ? (M + log2f(Ls)) * kTreeLn2 : -INFINITY;
 }
 
-// tc: the tcgen05 kernel.  `total` is what a caller is told, whichever kernel it is, so that it never shrinks as a problem grows.
-struct TreeLayout { int tc, S, row_tiles, tile_rows, pitch; size_t off_o, off_of, total; };
+// Row tiles of a unit of the tcgen05 kernel.  Two share the keys that they read; one makes twice as many units, which fill the SMs
+// better and end sooner.  us, one / two: 4 heads of 4 tiles x 216 keys 11.3 / 16.8, 64 of 2 x 3008 47 / 54, 8 of 2 x 33000 56 / 58,
+// 16 of 2 x 9000 42 / 40, 16 of 2 x 33000 118 / 95, 8 of 6 x 33000 150 / 135.
+static int tree_unit_tiles(int64_t heads, int tiles, int64_t keys) {
+    return tiles > 1 && (heads * tiles > kTreeTcCtas || (keys > 16000 && heads * tiles >= 32)) ? 2 : 1;
+}
+
+// How a call is carried out.  `total` is what a caller is told, whichever form it is, so that it never shrinks as a problem grows.
+struct TreeLayout {
+    int tc, R, runs, S, unit_tiles, units, pitch;
+    int64_t ctas;
+    size_t off_o, off_of, total;
+};
 
 static bool tree_layout(const lvlm_dims* d, int64_t cap, TreeLayout* L) {
     if (d->B <= 0 || d->H <= 0 || d->Hkv <= 0 || d->H % d->Hkv || d->T <= 0 || d->T > kTreeMaxT || d->H / d->Hkv > kTreeMaxGroup || cap <= 0) return false;
-    const int G = d->H / d->Hkv;
-    const int64_t heads = (int64_t)d->B * d->Hkv, rows = (int64_t)d->T * G;
-    const int64_t keys = (d->N > 0 && d->N < cap ? d->N : cap) + (d->draft_cap > 0 ? d->T : 0);
-    const int64_t mma_tiles = heads * ((rows + kTreeRows - 1) / kTreeRows);
-    L->tc = tree_uses_tc(d->T, rows, keys);
-    // the tcgen05 kernel: CTAs by the work there is at most, two slots each
-    const int64_t tc_tile = kTreeTcRows / G * G, tc_tiles = (rows + tc_tile - 1) / tc_tile;
-    const int64_t work = heads * tc_tiles * ((keys + kTreeTcRows - 1) / kTreeTcRows + 1) / kTreeTcLeast;
-    const int64_t tc_S = work < 1 ? 1 : work > kTreeTcCtas ? kTreeTcCtas : work;
-    L->pitch = (tc_tiles > 1 ? 2 : 1) * kTreeTcRows;
-    const int64_t places = tc_S > 1 ? 2 * tc_S * L->pitch : 0;
+    const int G = d->H / d->Hkv, rows = d->T * G;
+    const int64_t heads = (int64_t)d->B * d->Hkv;
+    const int64_t keys = d->N > 0 && d->N < cap ? d->N : cap;
+    const int drafts = d->draft_cap > 0 ? d->T : 0;
+    // tcgen05: units in as many parts as fill the SMs
+    const int tc_rows = kTreeTcRows / G * G, tiles = (rows + tc_rows - 1) / tc_rows;
+    const int64_t tc_steps = (keys + kTreeTcRows - 1) / kTreeTcRows + (drafts + kTreeTcRows - 1) / kTreeTcRows;
+    const int unit_tiles = tree_unit_tiles(heads, tiles, keys), tc_units = (tiles + unit_tiles - 1) / unit_tiles;
+    const int64_t units = heads * tc_units;
+    L->runs = units > kTreeTcCtas;
+    int64_t parts = L->runs ? 1 : kTreeTcCtas / units;
+    const int64_t most = tc_steps / 2;                       // (two key tiles or more a part: one, and more parts, is no faster)
+    parts = parts > most ? (most > 0 ? most : 1) : parts;
+    // mma.sync
+    const int R = (rows + kTreeRows - 1) / kTreeRows, room = R == 1 ? 2 * kTreeTcCtas : kTreeTcCtas;       // CTAs that run at a time
+    const int64_t stages = (keys + kTreeStageKeys - 1) / kTreeStageKeys + (drafts + kTreeStageKeys - 1) / kTreeStageKeys;
+    int S = 1;
+    while (S < kTreeMaxCluster && heads * 2 * S <= room && stages >= 2 * S) S *= 2;
+
+    // Estimates of either in us, fitted to caches of 100 to 33000 keys of 4 to 256 heads (10 % off): a stage a CTA of the one, a key tile a
+    // CTA of the other.  Measured, mma.sync / tcgen05: 16 rows or less, 4 heads x 3008 keys 10.8 / 13.0, x 9000 22 / 17; 16 heads x 9000
+    // 26 / 26; 64 heads x 9000 51 / 68; 17 to 32 rows, 8 heads x 1100 10.2 / 11.5, x 9000 27 / 20, 64 heads x 3008 35 / 33.
+    const int64_t waves = (heads * S + room - 1) / room, run = (stages + S - 1) / S;
+    const double mma_us = R == 1 ? 5 + (heads * S <= kTreeTcCtas ? 1.0 : 1.2) * waves * run : 7 + 1.13 * waves * run;
+    const double tc_us = 12 + 1.55 * (L->runs ? (double)heads * tiles * tc_steps / kTreeTcCtas : (double)((tc_steps + parts - 1) / parts) * unit_tiles);
+    L->tc = R > 2 || d->T > 32 * kTreeMmaWords || tc_us < mma_us;
+    L->R = R;
+    L->S = L->tc ? (int)parts : S;
+    L->unit_tiles = unit_tiles;
+    L->units = tc_units;
+    L->pitch = unit_tiles * kTreeTcRows;
+    L->ctas = !L->tc ? heads * S : L->runs ? kTreeTcCtas : units * parts;
+    const int64_t places = (int64_t)2 * kTreeTcCtas * (tiles > 1 ? 2 : 1) * kTreeTcRows;       // two slots a CTA
     L->off_o = align_up((size_t)places * 8, 256);
     L->off_of = L->off_o + (size_t)places * kHeadDim * 4;
-    L->total = align_up(L->off_of + (size_t)(heads * ((tc_tiles + 1) / 2)) * 8, 256);
-    // the other: clusters as large as the GPU has room for, a CTA with a stage of keys at least
-    int S = 1;
-    while (S < kTreeMaxCluster && mma_tiles * 2 * S <= kTreeTargetCtas && keys >= 2 * S * kTreeStageKeys) S *= 2;
-    L->S = L->tc ? (int)tc_S : S;
-    L->tile_rows = L->tc ? (int)tc_tile : kTreeRows;
-    L->row_tiles = (int)((rows + L->tile_rows - 1) / L->tile_rows);
+    L->total = align_up(L->off_of + (size_t)(heads * tiles) * 8, 256);
     return true;
+}
+
+template <int R>
+static lvlm_status launch_tree_mma(const TreeArgs& a, const TreeMaps& m, const TreeLayout& L, cudaStream_t stream) {
+    LVLM_RETURN_IF_CUDA(cudaFuncSetAttribute(tree_mma_kernel<R>, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynSmem));
+    return launch_kernel(tree_mma_kernel<R>, dim3((unsigned)L.ctas), dim3(TreeMma<R>::kThreads), TreeMma<R>::kSmem, stream, L.S, m.k, m.v, m.kd, m.vd, a);
 }
 
 size_t tree_attn_workspace(const lvlm_dims* d) {
@@ -439,31 +498,28 @@ extern "C" lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void*
     a.table = table; a.len = len; a.mask = mask; a.count = count;
     a.out = static_cast<__nv_bfloat16*>(out); a.lse = lse;
     a.B = d->B; a.H = d->H; a.G = d->H / d->Hkv; a.T = d->T; a.W = (d->T + 31) / 32; a.drafts = Kd != nullptr; a.mask_shared = d->mask_shared != 0;
-    a.S = L.S; a.row_tiles = L.row_tiles; a.tile_rows = L.tile_rows; a.pitch = L.pitch;
+    a.S = L.S; a.runs = L.runs; a.tile_rows = kTreeTcRows / a.G * a.G; a.unit_tiles = L.unit_tiles; a.units = L.units; a.pitch = L.pitch;
     a.scale_log2 = scale * kTreeLog2e;
     a.part_ml = reinterpret_cast<float2*>(wsb);
     a.part_o = reinterpret_cast<float*>(wsb + L.off_o);
     a.part_of = reinterpret_cast<int2*>(wsb + L.off_of);
     a.dev_status = dev_status;
-    const int64_t heads = (int64_t)d->B * d->Hkv, ctas = heads * L.row_tiles * L.S;
-    if (ctas > 0x7FFFFFFFll) return LVLM_ERR_UNSUPPORTED;
+    if (L.ctas > 0x7FFFFFFFll) return LVLM_ERR_UNSUPPORTED;
     lvlm_status st;
     if (L.tc) {
         const uint64_t dims[5] = {(uint64_t)kHeadDim, (uint64_t)a.G, (uint64_t)d->T, (uint64_t)d->Hkv, (uint64_t)d->B};
         const uint64_t strides[4] = {(uint64_t)a.q_sh * 2, (uint64_t)a.q_sn * 2, (uint64_t)a.G * a.q_sh * 2, (uint64_t)a.q_sb * 2};
         const uint32_t box[5] = {64, (uint32_t)a.G, (uint32_t)(kTreeTcRows / a.G), 1, 1};
         if (!make_tmap_bf16(&m.q, q, 5, dims, strides, box)) return LVLM_ERR_CUDA;
-        st = launch_tree_tc(a, m, stream);
+        st = launch_tree_tc(a, m, (int)L.ctas, stream);
     } else {
-        const size_t smem = 1024 + (size_t)kTreeStages * kTreeStageBytes;
-        LVLM_RETURN_IF_CUDA(cudaFuncSetAttribute(tree_mma_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynSmem));
-        return launch_kernel(tree_mma_kernel, dim3((unsigned)ctas), dim3(kTreeThreads), smem, stream, L.S, m.k, m.v, m.kd, m.vd, a);
+        return L.R == 1 ? launch_tree_mma<1>(a, m, L, stream) : launch_tree_mma<2>(a, m, L, stream);
     }
-    if (st != LVLM_OK || L.S == 1) return st;
+    if (st != LVLM_OK || (L.S == 1 && !L.runs)) return st;
     // a warp takes one group of channels where few units leave the GPU idle otherwise
-    const int64_t units = heads * ((L.row_tiles + 1) / 2);
+    const int64_t units = (int64_t)d->B * d->Hkv * L.units;
     const unsigned blocks = (unsigned)(L.pitch / 32);
-    if (units * blocks < 148)
+    if (units * blocks < kTreeTcCtas)
         return launch_kernel(tree_combine_kernel<1>, dim3((unsigned)units, blocks, 4), dim3(kTreeCombineWarps * 32), 0, stream, 1, a);
     return launch_kernel(tree_combine_kernel<4>, dim3((unsigned)units, blocks, 1), dim3(kTreeCombineWarps * 32), 0, stream, 1, a);
 }

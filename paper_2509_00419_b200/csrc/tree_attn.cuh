@@ -10,20 +10,23 @@ constexpr int kTreeMaxT = 256;                       // drafts a sequence: eight
 constexpr int kTreeMaxGroup = 64;
 constexpr int kTreeTcRows = 128;                     // rows of a tile of the tcgen05 kernel
 constexpr int kTreeTcCtas = 148;                     // its CTAs, one an SM
-constexpr int kTreeTcLeast = 4;                      // least work of one, in key tiles of a row tile (2 or more)
 constexpr float kTreeLog2e = 1.4426950408889634f, kTreeLn2 = 0.6931471805599453f;
 
 struct TreeArgs {
     const __nv_bfloat16* q; const int32_t* table; const int32_t* len; const uint32_t* mask; const int32_t* count;
     __nv_bfloat16* out; float* lse;
     int B, H, G, T, W, drafts, mask_shared;          // W mask words a row; drafts = 0: no Kd
-    int S, row_tiles;        // CTAs of a cluster (tcgen05 kernel: of the grid); tiles of its T G query rows
-    int tile_rows, pitch;    // query rows in a tile, and places for rows in a slot of the workspace
+    int S;                   // CTAs of a cluster; tcgen05 kernel: parts that the keys of a unit are cut into
+    // tcgen05 kernel:
+    int runs;                // the grid shares out the key tiles of all units instead
+    int tile_rows;           // query rows of a tile (row r = draft r / G, head r % G of the group)
+    int unit_tiles, units;   // row tiles of a unit of work (1 or 2); units of a head
+    int pitch;               // places for the rows of a unit in a slot of the workspace
     int64_t q_sb, q_sn, q_sh;
     float scale_log2;
-    // Partial results of the tcgen05 kernel.  A slot holds `pitch` rows, groups of four channels of all rows side by side; a CTA has two slots,
-    // for its first segment and its last; part_of [head, pair of row tiles]: the first slot of a unit, -1 = it was not cut, and how
-    // many more CTAs have a part of it, in their first slots.
+    // Partial results.  A slot holds `pitch` rows, groups of four channels of all rows side by side.  Slot (head, part, unit), or with runs
+    // two slots a CTA, for its first segment and its last, and part_of [head, unit]: the first slot of a unit, -1 = it was not
+    // cut, and how many more CTAs have a part of it, in their first slots.
     float2* part_ml;         // (max in the log2 domain, sum)
     float* part_o;           // output relative to that max
     int2* part_of;
@@ -34,18 +37,20 @@ struct TreeArgs {
 __device__ __forceinline__ void tree_flag(const TreeArgs& a, int bit) {
     if (a.dev_status) atomicOr(a.dev_status, bit);
 }
-__device__ __forceinline__ int tree_count(const TreeArgs& a, int b) {
-    if (!a.count) return a.T;
-    const int n = *(a.count + b);
-    if (n < 0 || n > a.T) { tree_flag(a, LVLM_DEV_BOUNDS); return 0; }
-    return n;
+// The drafts and the cache rows of a head (-1: its length is no length), and its steps of `keys` keys: of the cache, and in all.
+struct TreeHead { int n, ln, ns, nt; };
+__device__ __forceinline__ TreeHead tree_head(const TreeArgs& a, int hd, int keys) {
+    const int ln = __ldcg(a.len + hd), n = a.count ? __ldcg(a.count + hd / a.c.Hkv) : a.T;      // (both on their way before either is looked at)
+    TreeHead h;
+    h.n = n < 0 || n > a.T ? 0 : n;
+    h.ln = ln < 0 || ln > a.c.cap ? -1 : ln;
+    if (h.n != n || h.ln < 0) tree_flag(a, LVLM_DEV_BOUNDS);
+    h.ns = h.ln > 0 ? (h.ln + keys - 1) / keys : 0;
+    h.nt = h.ln < 0 ? 0 : h.ns + (a.drafts ? (h.n + keys - 1) / keys : 0);
+    return h;
 }
-// The cache rows of a head, -1: its length is no length.
-__device__ __forceinline__ int tree_len(const TreeArgs& a, int hd) {
-    const int ln = *(a.len + hd);
-    if (ln < 0 || ln > a.c.cap) { tree_flag(a, LVLM_DEV_BOUNDS); return -1; }
-    return ln;
-}
+// Steps in a part of a unit.
+__device__ __forceinline__ int tree_part(const TreeHead& h, int S) { return S == 1 ? max(h.nt, 1) : max(1, (h.nt + S - 1) / S); }
 
 // Word w of what draft t sees, limited to the n drafts there are.
 __device__ __forceinline__ uint32_t tree_see(const TreeArgs& a, int b, int t, int n, int w) {
@@ -58,6 +63,6 @@ __device__ __forceinline__ uint32_t tree_see(const TreeArgs& a, int b, int t, in
 }
 
 struct TreeMaps { CUtensorMap q, k, v, kd, vd; };
-lvlm_status launch_tree_tc(const TreeArgs& a, const TreeMaps& m, cudaStream_t stream);
+lvlm_status launch_tree_tc(const TreeArgs& a, const TreeMaps& m, int ctas, cudaStream_t stream);
 
 }  // namespace lvlm

@@ -7,9 +7,10 @@
 //   softmax          thread = query row, running maximum and sum in the log2 domain; probabilities go back as bf16 head + bf16
 //                    remainder over the logits they came from (a plain bf16 would cost as much again as the rounding of the result)
 //   O += P V_j       A = P from tensor memory, B = V as it lies in memory
-// One CTA an SM.  Lengths are ragged and only known on the device, so the key tiles of all units, weighted by what they take, are laid
-// end to end there and every CTA takes an equal run of them: a scheduler warp cuts the run into segments, a unit each, and the
-// other warps work through them without stopping in between (the keys of the next segment are fetched during the epilogue of this one).
+// One CTA an SM.  With fewer units than SMs a unit is cut into equal parts, a CTA each.  With more (a.runs), lengths being ragged and only
+// known on the device, the key tiles of all units, weighted by what they take, are laid end to end there and every CTA takes an
+// equal run of them: a scheduler warp cuts the run into segments, a unit each, and the other warps work through them without
+// stopping in between (the keys of the next segment are fetched during the epilogue of this one).
 // A unit that is cut leaves its parts (max, sum, output) in the workspace; tree_combine_kernel adds them in order.
 // Rows of V behind the end of the cache or of the drafts are zeroed in shared memory before they are multiplied: they may hold
 // anything, and their weight of zero would not stop a NaN.
@@ -32,24 +33,10 @@ static_assert(3 * kTRegsLaunch >= kTRegsFew + 2 * kTRegsMany, "the split has to 
 constexpr uint32_t kTTmemCols = 512;         // S/P of the two halves | O of the two halves
 constexpr float kTRescaleStep = 8.0f;
 
-// The key tiles and row tiles of a head; a head without keys has one tile of none, so that its rows are written.
-struct TreeHead { int n, ln, ns, nt, rt; };
-__device__ __forceinline__ TreeHead tree_head(const TreeArgs& a, int hd, int tt) {
-    const int ln = a.len[hd], n = a.count ? a.count[hd / a.c.Hkv] : a.T;      // (both on their way before either is looked at)
-    TreeHead h;
-    h.n = n < 0 || n > a.T ? 0 : n;
-    h.ln = ln < 0 || ln > a.c.cap ? -1 : ln;
-    if (h.n != n || h.ln != ln) tree_flag(a, LVLM_DEV_BOUNDS);
-    h.ns = h.ln > 0 ? (h.ln + kTT - 1) / kTT : 0;
-    h.nt = h.ln < 0 ? 0 : h.ns + (a.drafts ? (h.n + kTT - 1) / kTT : 0);
-    h.rt = h.n <= tt ? (h.n > 0) : (h.n + tt - 1) / tt;
-    return h;
-}
-// What a head weighs: a pair of row tiles 2 a key tile, an odd one 1.
-__device__ __forceinline__ int tree_weight(const TreeHead& h) { return max(h.nt, 1) * h.rt; }     // (far below 2^31: a tile is 64 KB)
-
+constexpr int kTLeast = 4;                   // least work of a CTA that shares, in key tiles of a row tile (2 or more)
+constexpr int kTWhole = 24;                  // a unit of no more work is not cut: its epilogue and the addition of its parts take longer
 constexpr int kTSegs = 4;                    // segments the scheduler is ahead at most
-struct TreeSeg { int hd, pair, t0, nk, split, n, ln, slot; };      // key tiles t0 .. t0 + nk - 1 of a unit; slot < 0: all of them; hd < 0: the end
+struct TreeSeg { int hd, tile, t0, nk, split, n, ln, slot; };      // row tile(s) `tile` (and the next), key tiles t0 .. t0 + nk - 1; slot < 0: all of them; hd < 0: the end
 
 struct TreeTcSmem {
     uint64_t seg_full[kTSegs], seg_empty[kTSegs], e_done, x_ready;
@@ -65,18 +52,21 @@ struct TreeTcSmem {
 
 // One short loop: the kernel runs through most of its code once, so that code fetched is time spent.
 __device__ __forceinline__ bool tree_wait(uint64_t* bar, uint32_t parity, TreeTcSmem* sm, const TreeArgs& a) {
-    const uint32_t addr = smem_u32(bar);
-#pragma unroll 1
-    for (uint32_t it = 0; it < kSpinLimit; ++it) {
-        if (mbar_try_for(addr, parity)) return true;
-        if (sm->abort) return false;
-    }
+    if (mbar_try(bar, parity)) return true;
+    if (sm->abort) return false;
+    if (mbar_wait(bar, parity)) return true;
     sm->abort = 1;
     tree_flag(a, LVLM_DEV_TIMEOUT);
     return false;
 }
 
-// grid.x = CTAs at most (one an SM)
+// Row tiles of a head that are asked for, and what it weighs: a pair of them 2 a key tile, an odd one 1 (far below 2^31: a tile is
+// 64 KB); a head without keys one tile, so that its rows are written.
+__device__ __forceinline__ int tree_rt(const TreeHead& h, int tt) { return h.n <= tt ? (h.n > 0) : (h.n + tt - 1) / tt; }
+__device__ __forceinline__ int tree_weight(const TreeHead& h, int tt) { return max(h.nt, 1) * tree_rt(h, tt); }
+
+// RUNS: the grid shares out the key tiles of all units; else a CTA has one part of one unit, and no scheduler
+template <bool RUNS>
 __global__ void __launch_bounds__(kTThreads, 1)
 tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
                const __grid_constant__ CUtensorMap kdmap, const __grid_constant__ CUtensorMap vdmap, const TreeArgs a) {
@@ -110,18 +100,33 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem_base = sm->tmem_base;
+    const uint32_t tmem_base = __shfl_sync(0xFFFFFFFFu, sm->tmem_base, 0);
     pdl_enter();
 
-    // ---- my run [lo, hi) of the weights of all heads, and the head it begins in ------------------------------------
     const int G = a.G, T = a.T, Hkv = a.c.Hkv, heads = a.B * Hkv, tt = kTT / G, me = blockIdx.x;      // tt drafts a row tile
+    const int pairs = a.units, ut = a.unit_tiles;
+    long long total = 0, per = 0, lo = 0, hi = 0;
+    if (!RUNS) {
+        if (threadIdx.x == 0) {                                   // a part of a unit a CTA: one segment
+            const int pair = me % pairs, part = me / pairs % a.S, hd = me / pairs / a.S;
+            const TreeHead h = tree_head(a, hd, kTT);
+            const int step = tree_part(h, a.S), t0 = part * step, rt = tree_rt(h, tt);
+            TreeSeg w;
+            w.hd = ut * pair < rt && (t0 < h.nt || part == 0) ? hd : -1;
+            w.tile = ut * pair; w.t0 = t0; w.nk = min(h.nt - t0, step); w.split = ut == 1 || ut * pair + 1 == rt; w.n = h.n; w.ln = h.ln;
+            w.slot = step >= h.nt ? -1 : me;
+            sm->seg[0] = w;
+        }
+        __syncthreads();
+    } else {
+    // ---- my run [lo, hi) of the weights of all heads, and the head it begins in ------------------------------------
     const int each = (heads + kTThreads - 1) / kTThreads, h_lo = min(heads, (int)threadIdx.x * each), h_hi = min(heads, h_lo + each);
     long long sum = 0;
     TreeHead head;
 #pragma unroll 1
     for (int hd = h_lo; hd < h_hi; ++hd) {
-        head = tree_head(a, hd, tt);
-        sum += tree_weight(head);
+        head = tree_head(a, hd, kTT);
+        sum += tree_weight(head, tt);
     }
     long long incl = sum;
 #pragma unroll
@@ -131,7 +136,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     }
     if (lane == 31) sm->scan[warp] = incl;
     __syncthreads();
-    long long total = 0, before = incl - sum;
+    long long before = incl - sum;
 #pragma unroll
     for (int w = 0; w < kTThreads / 32; ++w) {
         if (w < warp) before += sm->scan[w];
@@ -139,31 +144,34 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     }
     // equal runs, none so short that it is not worth a CTA's start
     const long long share = total >> 32 ? (total + gridDim.x - 1) / gridDim.x : (long long)(((uint32_t)total + gridDim.x - 1) / gridDim.x);
-    const long long per = max((long long)kTreeTcLeast, share), lo = min(total, per * me), hi = min(total, lo + per);
+    per = max((long long)kTLeast, share);
+    lo = min(total, per * me);
+    hi = min(total, lo + per);
     if (lo < hi && lo >= before && lo < before + sum) {
         long long p = before;
         int hd = h_lo;
         if (each > 1)
             for (;; ++hd) {
-                head = tree_head(a, hd, tt);
-                if (lo < p + tree_weight(head)) break;
-                p += tree_weight(head);
+                head = tree_head(a, hd, kTT);
+                if (lo < p + tree_weight(head, tt)) break;
+                p += tree_weight(head, tt);
             }
         sm->first_head = hd;
         sm->first_prefix = p;
         sm->first = head;
     }
     __syncthreads();
-    // the s-th segment of my run, for every warp but the scheduler
-    auto segment = [&](int s) -> TreeSeg {
-        TreeSeg x;
-        x.hd = -1;
-        if (__all_sync(0xFFFFFFFFu, tree_wait(&sm->seg_full[s % kTSegs], (s / kTSegs) & 1, sm, a))) {
-            x = sm->seg[s % kTSegs];
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sm->seg_empty[s % kTSegs]);
-        }
-        return x;
+    }
+    // the s-th segment of my run has been laid out: false where there is none
+    auto segment = [&](int s) -> bool {
+        if (!RUNS) return s == 0 && sm->seg[0].hd >= 0;
+        if (!__all_sync(0xFFFFFFFFu, tree_wait(&sm->seg_full[s % kTSegs], (s / kTSegs) & 1, sm, a))) return false;
+        return sm->seg[s % kTSegs].hd >= 0;
+    };
+    // and this warp does not read it any more
+    auto segment_done = [&](int s) {
+        __syncwarp();
+        if (RUNS && lane == 0) mbar_arrive(&sm->seg_empty[s % kTSegs]);
     };
 
     if (warp < 4) {
@@ -175,9 +183,10 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         int kc = 0, qc = 0;                                       // tiles and query tiles fetched for the segments before
         bool ok = true;
 #pragma unroll 1
-        for (int s = 0; ok; ++s) {
-            const TreeSeg w = segment(s);
-            if (w.hd < 0) break;
+        for (int s = 0; ok && (RUNS || s == 0); ++s) {
+            if (!segment(s)) break;
+            const TreeSeg w = sm->seg[s % kTSegs];
+            segment_done(s);
             const int b = w.hd / Hkv, g = w.hd % Hkv, ns = w.ln > 0 ? (w.ln + kTT - 1) / kTT : 0;
             // the page of my box of tile t; entries behind the head's length are not read: its last page again
             auto page_of = [&](int t) -> int {
@@ -197,8 +206,8 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                         const int nq = w.split ? 1 : 2;
                         mbar_arrive_expect_tx(&sm->q_full, (uint32_t)(nq * 2 * tt * G * 128));
                         for (int u = 0; u < nq; ++u) {
-                            tma_load_5d(sQ + u * kTTile, &qmap, &sm->q_full, 0, 0, (2 * w.pair + u) * tt, g, b);
-                            tma_load_5d(sQ + u * kTTile + kTHalf, &qmap, &sm->q_full, 64, 0, (2 * w.pair + u) * tt, g, b);
+                            tma_load_5d(sQ + u * kTTile, &qmap, &sm->q_full, 0, 0, (w.tile + u) * tt, g, b);
+                            tma_load_5d(sQ + u * kTTile + kTHalf, &qmap, &sm->q_full, 64, 0, (w.tile + u) * tt, g, b);
                         }
                     }
                     ++qc;
@@ -238,9 +247,13 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         int kc = 0, qc = 0, pc0 = 0, pc1 = 0;                     // of the segments before: key tiles, query tiles, tiles of either half
         bool ok = true;
 #pragma unroll 1
-        for (int s = 0; ok; ++s) {
-            const TreeSeg w = segment(s);
-            if (w.hd < 0) break;
+        for (int s = 0; ok && (RUNS || s == 0); ++s) {
+            if (!segment(s)) break;
+            TreeSeg w = sm->seg[s % kTSegs];
+            segment_done(s);
+            // (broadcast, so that the compiler knows them to be the same in every lane)
+            w.nk = __shfl_sync(0xFFFFFFFFu, w.nk, 0); w.split = __shfl_sync(0xFFFFFFFFu, w.split, 0);
+            w.t0 = __shfl_sync(0xFFFFFFFFu, w.t0, 0); w.ln = __shfl_sync(0xFFFFFFFFu, w.ln, 0); w.n = __shfl_sync(0xFFFFFFFFu, w.n, 0);
             if (w.nk == 0) continue;
             const int split = w.split, ns = w.ln > 0 ? (w.ln + kTT - 1) / kTT : 0;
             auto tiles_of = [&](int u) { return split ? (w.nk + 1 - u) / 2 : w.nk; };          // of half u
@@ -263,12 +276,11 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
             };
             // (the queries come once the epilogue before has read its output, so O may be written as well)
             ok = __all_sync(0xFFFFFFFFu, tree_wait(&sm->q_full, qc & 1, sm, a));
-#pragma unroll 1
+#pragma unroll
             for (int u = 0; u < 2; ++u)
                 if (ok && tiles_of(u) > 0) ok = issue_qk(u, 0);
-#pragma unroll 1
             for (int i = 0; ok && i < tiles_of(0); ++i) {
-#pragma unroll 1
+#pragma unroll
                 for (int u = 0; ok && u < 2; ++u) {
                     if (i >= tiles_of(u)) continue;
                     const int jl = split ? 2 * i + u : i, j = kc + jl, st = j % kTStages, t = w.t0 + jl;
@@ -313,35 +325,37 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
             kc += w.nk; ++qc;
             pc0 += tiles_of(0); pc1 += tiles_of(1);
         }
-    } else if (warp == 2) {
+    } else if (RUNS && warp == 2) {
         // ================= scheduler: cuts my run into segments =================
         long long at = lo, p = lo < hi ? sm->first_prefix : 0;    // how far I am; where head hd begins
         int hd = lo < hi ? sm->first_head : 0, s = 0;
         TreeHead h = sm->first;
         bool ok = true, first = true;
-        const int pairs = (a.row_tiles + 1) / 2;
         while (ok) {
             TreeSeg w;
             w.hd = -1;
             if (at < hi) {
-                const int nt = max(h.nt, 1), x = (int)(at - p);
-                if (x >= nt * h.rt) {
-                    p += nt * h.rt;
-                    h = tree_head(a, ++hd, tt);
+                const int nt = max(h.nt, 1), rt = tree_rt(h, tt), x = (int)(at - p);
+                if (x >= nt * rt) {
+                    p += nt * rt;
+                    h = tree_head(a, ++hd, kTT);
                     continue;
                 }
-                const int fp = h.rt / 2, pair = h.rt <= 2 ? 0 : min((int)((uint32_t)x / (uint32_t)(2 * nt)), fp), wt = pair < fp ? 2 : 1;
+                const int fp = rt / 2, pair = rt <= 2 ? 0 : min((int)((uint32_t)x / (uint32_t)(2 * nt)), fp), wt = pair < fp ? 2 : 1;
                 const long long u0 = p + pair * 2 * nt;           // where the unit begins; a tile weighs wt
-                const int t0 = ((int)(at - u0) + wt - 1) >> (wt - 1), left = (int)min((long long)(wt * nt), hi - u0), t1 = (left + wt - 1) >> (wt - 1);
+                // (a whole unit is the CTA's in whose run it begins)
+                const bool whole = wt * nt <= kTWhole;
+                const int left = (int)min((long long)(wt * nt), hi - u0);
+                const int t0 = whole ? (u0 < lo ? nt : 0) : ((int)(at - u0) + wt - 1) >> (wt - 1), t1 = whole ? nt : (left + wt - 1) >> (wt - 1);
                 at = u0 + wt * nt;
                 if (t0 >= t1) continue;
-                w.hd = hd; w.pair = pair; w.t0 = t0; w.nk = h.nt > 0 ? t1 - t0 : 0; w.split = wt == 1; w.n = h.n; w.ln = h.ln;
+                w.hd = hd; w.tile = 2 * pair; w.t0 = t0; w.nk = h.nt > 0 ? t1 - t0 : 0; w.split = wt == 1; w.n = h.n; w.ln = h.ln;
                 w.slot = t0 == 0 && t1 == nt ? -1 : 2 * me + (first ? 0 : 1);
                 first = false;
                 if (t0 == 0 && lane == 0) {
                     // where the parts of this unit lie: mine, then the first slots of the CTAs up to the one with its last tile
                     const long long z = u0 + wt * (nt - 1);
-                    a.part_of[(int64_t)hd * pairs + pair] = make_int2(w.slot, z < hi ? 0 : (int)((uint32_t)(z - lo) / (uint32_t)per));
+                    a.part_of[(int64_t)hd * pairs + pair] = make_int2(w.slot, w.slot < 0 ? 0 : (int)((uint32_t)(z - lo) / (uint32_t)per));
                 }
             }
             ok = s < kTSegs || __all_sync(0xFFFFFFFFu, tree_wait(&sm->seg_empty[s % kTSegs], ((s / kTSegs) - 1) & 1, sm, a));
@@ -362,20 +376,19 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         const f32x2 sc = both(a.scale_log2);
         int jc = 0, oc = 0, xc = 0;                              // of the segments before, or their parity: tiles of my half, outputs of half u (bit u), exchanges
 #pragma unroll 1
-        for (int s = 0;; ++s) {
-        const TreeSeg w = segment(s);
-        if (w.hd < 0) break;
-        const int split = w.split, n = w.n, tile = 2 * w.pair + (split ? 0 : u), b = w.hd / Hkv, g = w.hd % Hkv;
-        const int t = tile * tt + row / G;                       // my draft
-        const bool mine = row < tt * G && t < n;
-        const bool work = __any_sync(0xFFFFFFFFu, mine);         // a warp without rows only keeps the barriers going
-        const int n_mine = split ? (w.nk + 1 - u) / 2 : w.nk, n_other = split ? (w.nk + u) / 2 : w.nk;
-        const int ns = w.ln > 0 ? (w.ln + kTT - 1) / kTT : 0;
+        for (int s = 0; RUNS || s == 0; ++s) {
+        if (!segment(s)) break;
+        const TreeSeg& w = sm->seg[s % kTSegs];                   // (read where it is needed: registers are short)
+        const int split = w.split, n_mine = split ? (w.nk + 1 - u) / 2 : w.nk;
+        // a warp without rows only keeps the barriers going
+        const bool work = (quarter * 32 < tt * G) && (w.tile + (split ? 0 : u)) * tt + quarter * 32 / G < w.n;
+        int lim = w.ln - (w.t0 + (split ? u : 0)) * kTT;         // rows of the key tile that hold keys, 0 or less: it is one of the drafts
+        const int lim_step = split ? 2 * kTT : kTT;
         float m_used = -INFINITY;
         f32x2 l_run = both(0.f);
         bool ok = true;
 #pragma unroll 1
-        for (int j = 0; j < n_mine; ++j) {
+        for (int j = 0; j < n_mine; ++j, lim -= lim_step) {
             ok = __all_sync(0xFFFFFFFFu, tree_wait(&sm->s_full[u], (jc + j) & 1, sm, a));
             if (!ok) break;
             tc_fence_after();
@@ -387,14 +400,15 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
 #pragma unroll
             for (int c = 0; c < 4; ++c) tmem_ld32(s_addr + c * 32, v[c]);
             tmem_ld_wait();
-            const int kt = w.t0 + (split ? 2 * j + u : j);       // my key tile
-            const int lim = kt < ns ? w.ln - kt * kTT : 0;       // a tile of the cache: rows that hold keys, the same for all
             if (lim < kTT) {
+                const int ns = w.ln > 0 ? (w.ln + kTT - 1) / kTT : 0, t = (w.tile + (split ? 0 : u)) * tt + row / G, b = w.hd / Hkv;
+                const int w0 = (w.t0 + (split ? 2 * j + u : j) - ns) * (kTT / 32);       // the tile's first mask word
+                const bool mine = row < tt * G && t < w.n;
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
                     uint32_t bits;
-                    if (kt < ns) bits = lim >= c * 32 + 32 ? 0xFFFFFFFFu : lim <= c * 32 ? 0u : (1u << (lim - c * 32)) - 1u;
-                    else bits = mine ? tree_see(a, b, t, n, (kt - ns) * (kTT / 32) + c) : 0u;
+                    if (lim > 0) bits = lim >= c * 32 + 32 ? 0xFFFFFFFFu : lim <= c * 32 ? 0u : (1u << (lim - c * 32)) - 1u;
+                    else bits = mine ? tree_see(a, b, t, w.n, w0 + c) : 0u;
 #pragma unroll
                     for (int e = 0; e < 32; ++e) v[c][e] = (bits >> e) & 1u ? v[c][e] : -INFINITY;
                 }
@@ -450,7 +464,10 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
             }
             l_run = add2(l_run, add2(ps0, ps1));
         }
-        // ---- the rows: 64 channels at a time through shared memory (the Q tiles, which nobody needs any more) ---------------
+        // ---- the rows ------------------------------------------------------------------------------------------------------
+        const int n = w.n, tile = w.tile + (split ? 0 : u), b = w.hd / Hkv, g = w.hd % Hkv;
+        const int t = tile * tt + row / G;                       // my draft
+        const bool mine = row < tt * G && t < n;
         float l0, l1;
         unpack2(l_run, l0, l1);
         float l_row = l0 + l1, f0 = 1.f, f1 = 0.f;
@@ -462,6 +479,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 *reinterpret_cast<uint2*>(a.out + (((int64_t)b * T + td) * a.H + g * G + rr % G) * kHeadDim + lane * 4) = make_uint2(0u, 0u);
             }
             if (mine && a.lse && (!split || u == 0)) a.lse[((int64_t)b * a.H + g * G + row % G) * T + t] = -INFINITY;
+            segment_done(s);
             continue;
         }
         if (split) {
@@ -477,7 +495,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
             f1 = m1 > -INFINITY ? ex2_fast(m1 - m_used) : 0.f;
             l_row = sm->xl[0][row] * f0 + sm->xl[1][row] * f1;
             ok = ok && (n_mine == 0 || tree_wait(&sm->o_done[u], (oc >> u) & 1, sm, a));
-            ok = ok && (n_other == 0 || tree_wait(&sm->o_done[u ^ 1], (oc >> (u ^ 1)) & 1, sm, a));
+            ok = ok && ((w.nk + u) / 2 == 0 || tree_wait(&sm->o_done[u ^ 1], (oc >> (u ^ 1)) & 1, sm, a));
         } else {
             ok = ok && tree_wait(&sm->o_done[u], (oc >> u) & 1, sm, a);
         }
@@ -539,6 +557,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         fence_proxy_async();
         tc_fence_before();
         __syncwarp();
+        segment_done(s);
         if (lane == 0) mbar_arrive(&sm->e_done);
         }
     }
@@ -554,15 +573,20 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     }
 }
 
-lvlm_status launch_tree_tc(const TreeArgs& a, const TreeMaps& m, cudaStream_t stream) {
+template <bool RUNS>
+static lvlm_status launch_tree_tc(const TreeArgs& a, const TreeMaps& m, int ctas, cudaStream_t stream) {
     const size_t smem = 1024 + (size_t)kTTile * (2 + 2 * kTStages) + sizeof(TreeTcSmem);
-    LVLM_RETURN_IF_CUDA(cudaFuncSetAttribute(tree_tc_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
+    LVLM_RETURN_IF_CUDA(cudaFuncSetAttribute(tree_tc_kernel<RUNS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     static const int regs = [] {
         cudaFuncAttributes f;
-        return cudaFuncGetAttributes(&f, tree_tc_kernel) == cudaSuccess ? f.numRegs : 0;
+        return cudaFuncGetAttributes(&f, tree_tc_kernel<RUNS>) == cudaSuccess ? f.numRegs : 0;
     }();
     if (3 * regs < kTRegsFew + 2 * kTRegsMany) return LVLM_ERR_CUDA;       // the split would wait for registers that nobody has
-    return launch_kernel(tree_tc_kernel, dim3((unsigned)a.S), dim3(kTThreads), smem, stream, 1, m.q, m.k, m.v, m.kd, m.vd, a);
+    return launch_kernel(tree_tc_kernel<RUNS>, dim3((unsigned)ctas), dim3(kTThreads), smem, stream, 1, m.q, m.k, m.v, m.kd, m.vd, a);
+}
+
+lvlm_status launch_tree_tc(const TreeArgs& a, const TreeMaps& m, int ctas, cudaStream_t stream) {
+    return a.runs ? launch_tree_tc<true>(a, m, ctas, stream) : launch_tree_tc<false>(a, m, ctas, stream);
 }
 
 }  // namespace lvlm
