@@ -351,7 +351,7 @@ lvlm_status lvlm_decode_attn_static(const void* q, void* Kc, void* Vc, int32_t* 
  *   len_out[b,g]          = len[b,g] + count[b]
  *   pos        [axes][B][T] int32, positions of the tokens; one outside [0, n_pos) sets LVLM_DEV_BOUNDS and leaves the
  *              channels that follow it as they are
- *   cos_sin    [n_pos][rot] fp32; cos_sin and pos are only needed with rot > 0
+ *   cos_sin    [n_pos][rot] fp32, 16-byte aligned; cos_sin and pos are only needed with rot > 0
  *   len        [B][Hkv] int32, or NULL: all zero (a draft cache)
  *   len_out    optional [B][Hkv] int32, may be len itself (a second small launch then where T > 1)
  *   acc_score  optional [B][Hkv][cap] fp32: the new entries become 0, as lvlm_decode_attn starts them

@@ -377,13 +377,10 @@ def _rows(t: torch.Tensor, name: str, shape, strides, device: int):
 
 
 def _outer(t: torch.Tensor, name: str, strides, n: int):
-    """The first n strides for the C call: 0 (packed) for a dimension of one element, whose stride means nothing."""
-    lead = strides[:n]
-    odd = 0
-    for x in lead:
-        odd |= x & 7 if x else 7
-    if not odd:
-        return lead
+    """The first n strides (2 or 3) for the C call: 0 (packed) for a dimension of one element, whose stride means nothing."""
+    a, b, c = strides[0], strides[1], strides[n - 1]
+    if a and b and c and not (a | b | c) & 7:
+        return strides[:n]
     st = tuple([x if size > 1 else 0 for x, size in zip(strides[:n], t.shape)])
     if any(x == 0 and size > 1 for x, size in zip(st, t.shape)):
         raise ValueError(f"{name} repeats its elements along a dimension (an expanded view)")
@@ -408,8 +405,7 @@ def _cache(d: Dims, Kc, Vc, table, B, Hkv, D, device: int):
     if len(shape) != 3 or len(t_shape) != 3:
         raise ValueError("a paged cache has the shape [n_pages, page, D], its table [B, Hkv, max_pages]")
     d.n_pages, d.page, _ = shape
-    page_stride = st[0]
-    d.page_stride = page_stride if page_stride and not page_stride & 7 else _outer(Kc, "Kc", st, 1)[0]
+    d.page_stride = _outer(Kc, "Kc", st, 2)[0]
     d.max_pages = n = t_shape[2]
     return kp, vp, _arg(table, "table", _I32, (B, Hkv, n), device)
 
@@ -511,7 +507,7 @@ def rope_append(k_new, v_new, pos, cos_sin, Kc, Vc, length=None, *, q=None, q_ou
     _check(lib().lvlm_rope_append(
         qp, knp, vnp, _arg(pos, "pos", _I32, pos_shape, dev), _arg(cos_sin, "cos_sin", _F32, None, dev),
         _arg(count, "count", _I32, (B,), dev), qop, kp, vp, tp, lp, lp if len_out is None else _arg(len_out, "len_out", _I32, hs, dev),
-        ap, pcp, ctypes.byref(d), _arg(dev_status, "dev_status", _I32, None, dev), _stream(stream)), "lvlm_rope_append")
+        ap, pcp, ctypes.byref(d), _arg(dev_status, "dev_status", _I32, None, dev), torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream), "lvlm_rope_append")
     return q_out
 
 
@@ -538,7 +534,7 @@ def commit_rows(Kd, Vd, Kc, Vc, length, count=None, *, index=None, table=None, l
     _check(lib().lvlm_commit_rows(
         kdp, vdp, _arg(index, "index", _I32, (B, T), dev), _arg(count, "count", _I32, hs if d.count_heads else (B,), dev),
         _arg(pos, "pos", _I32, (B, rows), dev), kp, vp, tp, lp, lp if len_out is None else _arg(len_out, "len_out", _I32, hs, dev),
-        ap, pcp, ctypes.byref(d), _arg(dev_status, "dev_status", _I32, None, dev), _stream(stream)), "lvlm_commit_rows")
+        ap, pcp, ctypes.byref(d), _arg(dev_status, "dev_status", _I32, None, dev), torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream), "lvlm_commit_rows")
 
 
 def tree_dims(q, Kc, table=None, Kd=None, *, max_len=None) -> Dims:
@@ -592,5 +588,5 @@ def tree_attn(q, Kc, Vc, length, *, Kd=None, Vd=None, mask=None, count=None, tab
     _check(lib().lvlm_tree_attn(qp, kp, vp, tp, _arg(length, "length", _I32, (B, Hkv), dev), kdp, vdp, mp,
                                 _arg(count, "count", _I32, (B,), dev), ctypes.byref(d), scale, _arg(out, "out", _BF16, shape, dev),
                                 _arg(lse, "lse", _F32, (B, H, T), dev), ws.data_ptr(), ws.numel() * ws.element_size(),
-                                _arg(dev_status, "dev_status", _I32, None, dev), _stream(stream)), "lvlm_tree_attn")
+                                _arg(dev_status, "dev_status", _I32, None, dev), torch._C._cuda_getCurrentRawStream(dev) if stream is None else stream.cuda_stream), "lvlm_tree_attn")
     return out, lse

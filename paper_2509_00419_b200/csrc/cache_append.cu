@@ -8,11 +8,15 @@
 
 namespace lvlm {
 
-constexpr int kRopeThreads = 256;
 constexpr int kRowLanes = 8;                       // lanes of a 256-byte row: two 16-byte chunks each
-constexpr int kRopeGroups = kRopeThreads / kRowLanes;
+// Threads of a CTA, a token.  Many tokens: two warps, each with many rows after one wait for the positions, and 18 CTAs an SM; a token
+// or a few: all rows at once.  us with 64 / 256 threads: 26200 tokens of 48 rows 100 / 164 (the bytes at the copy rate: 96), 16640 of
+// 64 rows 87 / 115 (84); one token 3.6 / 2.7, 208 tokens of 48 rows 4.4 / 3.3.
+constexpr int kRopeMany = 64, kRopeFew = 256, kRopeFewTokens = 2 * 148;
 constexpr int kCommitThreads = 256;
-constexpr int kCommitRows = 64;                    // rows of K and of V a CTA moves
+// Rows of K and of V a CTA moves.  A CTA waits for three loads, one behind the other (length, page, row), so it is many CTAs that keep
+// HBM busy: 8 an SM.  570 MB: 107 us with 64 rows a CTA, 95 with 32, 90.6 with their registers cut to fit 8 (the copy rate: 86).
+constexpr int kCommitRows = 32;
 
 struct RopeArgs {
     const __nv_bfloat16* q; const __nv_bfloat16* k_new; const __nv_bfloat16* v_new;
@@ -67,14 +71,17 @@ __device__ __forceinline__ void turn_neighbours(uint4& x, uint4& y, const float*
     y = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
-// grid.x = B * T tokens.  A token's rows are its H queries, Hkv keys and Hkv values; a group of 8 lanes takes every 32nd row,
-// with its eight frequencies' cosines and sines in registers for all of them.
-__global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeArgs a) {
+// grid.x = B * T tokens.  A token's rows are its H queries, Hkv keys and Hkv values, shared out to groups of 8 lanes; a group takes two
+// at a time, so that their loads overlap, with its eight frequencies' cosines and sines in registers for all of them.
+template <int THREADS>
+__global__ void __launch_bounds__(THREADS, THREADS == kRopeMany ? 18 : 1) rope_append_kernel(const RopeArgs a) {
+    constexpr int kGroups = THREADS / kRowLanes;
     pdl_enter();
     const int lane8 = threadIdx.x & (kRowLanes - 1), group = threadIdx.x / kRowLanes;
-    const int b = blockIdx.x / a.T, t = blockIdx.x % a.T, Hkv = a.c.Hkv;
+    const int b = blockIdx.x / a.T, t = blockIdx.x % a.T, Hkv = a.c.Hkv, rows = a.H + 2 * Hkv;
     const int n = checked_count(a.count, b, a.T, a.dev_status);
     const bool live = t < n;
+    if (!live && !(a.bump && t == 0)) return;
 
     // chunks of 16 bytes: c0 and c1 are a rotated pair of chunks, or two that stay
     const int half = a.rot / 16;                   // chunks of the first half of the rotated channels
@@ -84,49 +91,78 @@ __global__ void __launch_bounds__(kRopeThreads) rope_append_kernel(const RopeArg
     float cs[8], sn[8];
     if (turned && live) {
         const int f0 = lane8 * 8;                  // my frequencies f0 .. f0 + 7
+        auto axis_of = [&](int f) -> int { return a.axes == 3 ? (f >= a.sect0) + (f >= a.sect0 + a.sect1) : 0; };
+        auto position = [&](int axis) -> int {
+            const int p = a.pos[((int64_t)axis * a.B + b) * a.T + t];
+            if (p >= 0 && p < a.n_pos) return p;
+            flag_bounds(a.dev_status);
+            return -1;
+        };
+        if (axis_of(f0) == axis_of(f0 + 7)) {
+            const int p = position(axis_of(f0));
+            const float4* c4 = reinterpret_cast<const float4*>(a.cos_sin + (int64_t)(p < 0 ? 0 : p) * a.rot + f0);
+            const float4* s4 = c4 + a.rot / 8;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int axis = a.axes == 3 ? (f0 + i >= a.sect0) + (f0 + i >= a.sect0 + a.sect1) : 0;
-            const int p = *(a.pos + ((int64_t)axis * a.B + b) * a.T + t);
-            const bool ok = p >= 0 && p < a.n_pos;
-            if (!ok) flag_bounds(a.dev_status);
-            const float* row = a.cos_sin + (int64_t)(ok ? p : 0) * a.rot + f0 + i;
-            cs[i] = ok ? *row : 1.f;
-            sn[i] = ok ? *(row + a.rot / 2) : 0.f;
+            for (int i = 0; i < 2; ++i) {
+                const float4 c = p < 0 ? make_float4(1.f, 1.f, 1.f, 1.f) : c4[i], s = p < 0 ? make_float4(0.f, 0.f, 0.f, 0.f) : s4[i];
+                cs[4 * i] = c.x; cs[4 * i + 1] = c.y; cs[4 * i + 2] = c.z; cs[4 * i + 3] = c.w;
+                sn[4 * i] = s.x; sn[4 * i + 1] = s.y; sn[4 * i + 2] = s.z; sn[4 * i + 3] = s.w;
+            }
+        } else {                                   // a section ends among them
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int p = position(axis_of(f0 + i));
+                const float* row = a.cos_sin + (int64_t)(p < 0 ? 0 : p) * a.rot + f0 + i;
+                cs[i] = p < 0 ? 1.f : row[0];
+                sn[i] = p < 0 ? 0.f : row[a.rot / 2];
+            }
         }
     }
-    for (int r = group; r < a.H + 2 * Hkv; r += kRopeGroups) {
-        const __nv_bfloat16* from;
-        __nv_bfloat16* to;
-        bool turns = turned;
-        if (r < a.H) {
-            if (!a.q || !live) continue;
-            from = a.q + (int64_t)b * a.q_sb + (int64_t)t * a.q_sn + (int64_t)r * a.q_sh;
-            to = a.q_out + (int64_t)b * a.qo_sb + (int64_t)t * a.qo_sn + (int64_t)r * a.qo_sh;
-        } else {
-            const bool key = r < a.H + Hkv;
-            const int g = r - a.H - (key ? 0 : Hkv);
-            const int64_t hd = (int64_t)b * Hkv + g;
-            const int ln = checked_start(a.len, hd, n, a.c.cap, a.dev_status);
-            if (a.bump && key && t == 0 && lane8 == 0) a.len_out[hd] = ln >= 0 ? ln + n : a.len ? a.len[hd] : 0;
-            if (ln < 0 || !live) continue;
-            const int64_t off = cache_row(a.c, a.table, b, g, ln + t);
-            if (off < 0) { flag_bounds(a.dev_status); continue; }
-            if (key && lane8 == 0) {
-                if (a.acc_score) a.acc_score[hd * a.c.cap + ln + t] = 0.f;
-                if (a.pos_cache) a.pos_cache[hd * a.c.cap + ln + t] = a.pos[(int64_t)b * a.T + t];
+    for (int r0 = group; r0 < rows; r0 += 2 * kGroups) {
+        uint4 x[2], y[2];
+        __nv_bfloat16* to[2];
+        bool turns[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int r = r0 + u * kGroups;
+            to[u] = nullptr;
+            if (r >= rows) continue;
+            const __nv_bfloat16* from;
+            turns[u] = turned;
+            if (r < a.H) {
+                if (!live) continue;
+                from = a.q + (int64_t)b * a.q_sb + (int64_t)t * a.q_sn + (int64_t)r * a.q_sh;
+                to[u] = a.q_out + (int64_t)b * a.qo_sb + (int64_t)t * a.qo_sn + (int64_t)r * a.qo_sh;
+            } else {
+                const bool key = r < a.H + Hkv;
+                const int g = r - a.H - (key ? 0 : Hkv);
+                const int64_t hd = (int64_t)b * Hkv + g;
+                const int ln = checked_start(a.len, hd, n, a.c.cap, a.dev_status);
+                if (a.bump && key && t == 0 && lane8 == 0) a.len_out[hd] = ln >= 0 ? ln + n : a.len ? a.len[hd] : 0;
+                if (ln < 0 || !live) continue;
+                const int64_t off = cache_row(a.c, a.table, b, g, ln + t);
+                if (off < 0) { flag_bounds(a.dev_status); continue; }
+                if (key && lane8 == 0) {
+                    if (a.acc_score) a.acc_score[hd * a.c.cap + ln + t] = 0.f;
+                    if (a.pos_cache) a.pos_cache[hd * a.c.cap + ln + t] = a.pos[(int64_t)b * a.T + t];
+                }
+                from = (key ? a.k_new : a.v_new) + (int64_t)b * a.n_sb + (int64_t)t * a.n_sn + (int64_t)g * a.n_sh;
+                to[u] = (key ? a.Kc : a.Vc) + off;
+                turns[u] = turned && key;
             }
-            from = (key ? a.k_new : a.v_new) + (int64_t)b * a.n_sb + (int64_t)t * a.n_sn + (int64_t)g * a.n_sh;
-            to = (key ? a.Kc : a.Vc) + off;
-            turns = turned && key;
+            x[u] = reinterpret_cast<const uint4*>(from)[c0];
+            y[u] = reinterpret_cast<const uint4*>(from)[c1];
         }
-        uint4 x = reinterpret_cast<const uint4*>(from)[c0], y = reinterpret_cast<const uint4*>(from)[c1];
-        if (turns) {
-            if (a.interleaved) turn_neighbours(x, y, cs, sn);
-            else turn(x, y, cs, sn);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if (!to[u]) continue;
+            if (turns[u]) {
+                if (a.interleaved) turn_neighbours(x[u], y[u], cs, sn);
+                else turn(x[u], y[u], cs, sn);
+            }
+            reinterpret_cast<uint4*>(to[u])[c0] = x[u];
+            reinterpret_cast<uint4*>(to[u])[c1] = y[u];
         }
-        reinterpret_cast<uint4*>(to)[c0] = x;
-        reinterpret_cast<uint4*>(to)[c1] = y;
     }
 }
 
@@ -153,7 +189,7 @@ struct CommitArgs {
 };
 
 // grid (heads, runs of kCommitRows rows): 16 lanes move a row of K and the row of V of the same number.
-__global__ void __launch_bounds__(kCommitThreads) commit_rows_kernel(const CommitArgs a) {
+__global__ void __launch_bounds__(kCommitThreads, 8) commit_rows_kernel(const CommitArgs a) {
     pdl_enter();
     const int Hkv = a.c.Hkv, hd = blockIdx.x, b = hd / Hkv, g = hd % Hkv;
     const int n = checked_count(a.count, a.count_heads ? hd : b, a.T, a.dev_status);
@@ -230,7 +266,7 @@ extern "C" lvlm_status lvlm_rope_append(const void* q, const void* k_new, const 
     a.n_sh = d->new_stride_h ? d->new_stride_h : d->D;
     a.n_sn = d->new_stride_n ? d->new_stride_n : (int64_t)d->Hkv * d->D;
     a.n_sb = d->new_stride_b ? d->new_stride_b : (int64_t)d->T * a.n_sn;
-    if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out) || !aligned16(Kc) || !aligned16(Vc) ||
+    if (!aligned16(cos_sin) || !aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(q_out) || !aligned16(Kc) || !aligned16(Vc) ||
         a.q_sh % 8 || a.q_sn % 8 || a.q_sb % 8 || a.n_sh % 8 || a.n_sn % 8 || a.n_sb % 8)
         return LVLM_ERR_ALIGNMENT;
     if (q && q_out != q &&
@@ -250,7 +286,8 @@ extern "C" lvlm_status lvlm_rope_append(const void* q, const void* k_new, const 
     const bool in_place = len_out != nullptr && len_out == len;
     a.bump = len_out != nullptr && !in_place;
     a.dev_status = dev_status;
-    const lvlm_status st = launch_kernel(rope_append_kernel, dim3((unsigned)tokens), dim3(kRopeThreads), 0, stream, 1, a);
+    const lvlm_status st = tokens <= kRopeFewTokens ? launch_kernel(rope_append_kernel<kRopeFew>, dim3((unsigned)tokens), dim3(kRopeFew), 0, stream, 1, a)
+                                                    : launch_kernel(rope_append_kernel<kRopeMany>, dim3((unsigned)tokens), dim3(kRopeMany), 0, stream, 1, a);
     if (st != LVLM_OK || !in_place) return st;
     return grow_len(len_out, count, 0, (int)heads, a.c, d->T, stream);
 }

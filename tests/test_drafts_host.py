@@ -141,7 +141,7 @@ def test_rope_append_refusals(lib):
     for page in (8, 48):
         assert call(_dims(**{**PAGED, "page": page}), table=P) == L.ERR_UNSUPPORTED
     assert call(_dims(page=1 << 20, n_pages=4, max_pages=1 << 12), table=P) == L.ERR_UNSUPPORTED      # a capacity beyond 32 bits
-    for kw in (dict(q=ODD), dict(k=ODD), dict(v=ODD), dict(q_out=ODD), dict(K=ODD), dict(V=ODD)):
+    for kw in (dict(q=ODD), dict(k=ODD), dict(v=ODD), dict(q_out=ODD), dict(K=ODD), dict(V=ODD), dict(cs=ODD)):
         assert call(_dims(), **kw) == L.ERR_ALIGNMENT, kw
     for kw in (dict(q_stride_n=1028), dict(new_stride_h=132), dict(kv_stride_h=100 * 128 + 4)):
         assert call(_dims(**kw)) == L.ERR_ALIGNMENT, kw
