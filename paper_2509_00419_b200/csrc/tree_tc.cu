@@ -259,7 +259,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
             auto tiles_of = [&](int u) { return split ? (w.nk + 1 - u) / 2 : w.nk; };          // of half u
             auto issue_qk = [&](int u, int i) -> bool {
                 const int j = kc + (split ? 2 * i + u : i), st = j % kTStages;
-                if (!__all_sync(0xFFFFFFFFu, tree_wait(&sm->k_full[st], (j / kTStages) & 1, sm, a))) return false;
+                if ((split || u == 0) && !__all_sync(0xFFFFFFFFu, tree_wait(&sm->k_full[st], (j / kTStages) & 1, sm, a))) return false;
                 tc_fence_after();
                 const uint64_t qd = qd0 + (uint32_t)((split ? 0 : u) * (kTTile >> 4)), kd = kd0 + (uint32_t)(st * (kTTile >> 4));
                 if (elect_one()) {
@@ -286,7 +286,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                     const int jl = split ? 2 * i + u : i, j = kc + jl, st = j % kTStages, t = w.t0 + jl;
                     const uint64_t vd = vd0 + (uint32_t)(st * (kTTile >> 4));
                     const uint32_t p_tmem = tmem_base + u * kTT, o_tmem = tmem_base + (2 + u) * kTT;
-                    ok = __all_sync(0xFFFFFFFFu, tree_wait(&sm->v_full[st], (j / kTStages) & 1, sm, a));
+                    ok = (!split && u == 1) || __all_sync(0xFFFFFFFFu, tree_wait(&sm->v_full[st], (j / kTStages) & 1, sm, a));
                     if (!ok) break;
                     if (split || u == 0) {
                         // rows of the tile that hold keys, rows that hold anything (drafts: the copy has zeroed those from T on)

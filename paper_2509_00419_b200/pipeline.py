@@ -184,6 +184,71 @@ class DecodeLayers:
         return int(self.len.sum().item()) * 128 * 2 * 2
 
 
+class PagedLayers:
+    """KV caches of several layers in one pool of pages, ragged per (layer, sequence, KV head): what a compression evicts is free
+    memory.  ``pack`` takes over the contiguous caches of a ``DecodeLayers``; a step then runs, per layer, a tree of up to T
+    drafted tokens (``draft_layer``: rotation, draft cache, attention over cache and drafts), and ``commit`` appends the accepted ones
+    of all layers.  A head's pages are handed out by ``reserve`` on the host, ahead of the rows that need them."""
+
+    def __init__(self, n_layers, B, H, Hkv, n_pages, page, max_pages, T, device, rot=128):
+        self.nl, self.B, self.H, self.Hkv, self.page, self.T, self.rot, self.device = n_layers, B, H, Hkv, page, T, rot, device
+        bf, i32 = torch.bfloat16, torch.int32
+        self.K = torch.empty(n_pages, page, 128, dtype=bf, device=device)
+        self.V = torch.empty(n_pages, page, 128, dtype=bf, device=device)
+        self.table = torch.full((n_layers, B, Hkv, max_pages), -1, dtype=i32, device=device)
+        self.len = torch.zeros(n_layers, B, Hkv, dtype=i32, device=device)
+        self.Kd = torch.empty(n_layers, B, Hkv, T, 128, dtype=bf, device=device)
+        self.Vd = torch.empty(n_layers, B, Hkv, T, 128, dtype=bf, device=device)
+        self.q = torch.empty(B, T, H, 128, dtype=bf, device=device)
+        self.out = torch.empty(n_layers, B, T, H, 128, dtype=bf, device=device)
+        self.status = torch.zeros(1, dtype=i32, device=device)
+        d = L.tree_dims(self.q, self.K, self.table[0], self.Kd[0])
+        self.ws = L.alloc_workspace(L.OP_TREE_ATTN, d, device)
+        self._free = list(range(n_pages - 1, -1, -1))
+        self._held = torch.zeros(n_layers, B, Hkv, dtype=torch.int64)      # pages of each head
+        self._table = torch.full((n_layers, B, Hkv, max_pages), -1, dtype=i32)
+
+    def reserve(self, rows: torch.Tensor):
+        """Pages for ``rows`` [layer][B][Hkv] rows a head (on the host): hands out what is missing."""
+        need = (rows.to(torch.int64) + self.page - 1) // self.page
+        if int(need.max()) > self._table.shape[3]:
+            raise ValueError(f"a head needs {int(need.max())} pages, its table has {self._table.shape[3]} entries")
+        missing = (need - self._held).clamp_min(0)
+        if int(missing.sum()) > len(self._free):
+            raise RuntimeError(f"{int(missing.sum())} pages are missing, {len(self._free)} are free")
+        for l, b, g in missing.nonzero().tolist():
+            for j in range(int(self._held[l, b, g]), int(need[l, b, g])):
+                self._table[l, b, g, j] = self._free.pop()
+        self._held = torch.maximum(self._held, need)
+        self.table.copy_(self._table)
+
+    def pages_free(self) -> int:
+        return len(self._free)
+
+    def pack(self, src: "DecodeLayers", extra: int = 0):
+        """Moves the contiguous caches of ``src`` into pages, with room for ``extra`` rows more a head.  The lengths are read back."""
+        self.reserve(src.len.cpu() + extra)
+        shp = (self.nl * self.B, self.Hkv)
+        self.len.zero_()
+        L.commit_rows(src.K.view(*shp, src.cap, 128), src.V.view(*shp, src.cap, 128), self.K, self.V, self.len.view(shp),
+                      src.len.view(shp), table=self.table.view(*shp, -1), dev_status=self.status)
+
+    def draft_layer(self, l, q, k, v, pos, cos_sin, mask=None, count=None, sections=None, max_len=None):
+        """One layer of a step: q [B][T][H][128], k, v [B][T][Hkv][128] of the drafts at the positions pos [B][T].  Returns the
+        attention's output [B][T][H][128]."""
+        L.rope_append(k, v, pos, cos_sin, self.Kd[l], self.Vd[l], q=q, q_out=self.q, count=count, sections=sections,
+                      dev_status=self.status)
+        out, _ = L.tree_attn(self.q, self.K, self.V, self.len[l], Kd=self.Kd[l], Vd=self.Vd[l], mask=mask, count=count,
+                             table=self.table[l], out=self.out[l], max_len=max_len, ws=self.ws, dev_status=self.status)
+        return out
+
+    def commit(self, index, count):
+        """Appends the drafts index [B][T] (the accepted path), ``count`` [B] of them, to the caches of all layers."""
+        shp = (self.nl * self.B, self.Hkv)
+        L.commit_rows(self.Kd.view(*shp, self.T, 128), self.Vd.view(*shp, self.T, 128), self.K, self.V, self.len.view(shp),
+                      count.repeat(self.nl), index=index.repeat(self.nl, 1), table=self.table.view(*shp, -1), dev_status=self.status)
+
+
 def capture(fn, warmup=1):
     """Runs ``fn`` eagerly ``warmup`` times, then captures it into a CUDA graph."""
     s = torch.cuda.Stream()

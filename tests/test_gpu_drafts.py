@@ -452,3 +452,154 @@ def test_binding_refuses_what_the_call_cannot_see():
     with pytest.raises(L.LvlmError):
         L.commit_rows(z, z, z, z.clone(), i)
     assert (i == 0).all()
+
+
+# ---- as they are used together -------------------------------------------------------------------------------------
+def test_drafts_over_a_compressed_cache():
+    """Compression, the caches into pages, two steps of trees, each with its accepted path committed: every output and every
+    cache row against the oracle, and a plain decode step over the result."""
+    from oracle import lvlm_oracle as O
+    from paper_2509_00419_b200 import pipeline as P
+    r = np.random.default_rng(21)
+    nl, B, H, Hkv, cap, T, page = 2, 3, 8, 2, 96, 9, 16
+    src = P.DecodeLayers(nl, B, H, Hkv, cap, "cuda")
+    K, V = bf(r, nl, B, Hkv, cap, 128), bf(r, nl, B, Hkv, cap, 128)
+    acc = r.random((nl, B, Hkv, cap)).astype(np.float32)
+    ln = r.integers(60, cap + 1, size=(nl, B, Hkv)).astype(np.int32)
+    src.K.copy_(K); src.V.copy_(V); src.acc.copy_(torch.from_numpy(acc)); src.len.copy_(torch.from_numpy(ln))
+    src.compress(beta=0.7)
+    shp = (nl * B, Hkv)
+    want = O.kv_compress(f64(K).reshape(*shp, cap, 128), f64(V).reshape(*shp, cap, 128), acc.reshape(*shp, cap), ln.reshape(shp), beta=0.7)
+    length = want["len"].reshape(nl, B, Hkv).copy()
+    assert np.array_equal(i32(src.len), length) and length.min() < length.max()
+    used = int(((length + 2 * T + page - 1) // page).sum())
+    new = P.PagedLayers(nl, B, H, Hkv, used, page, (cap + 2 * T + page - 1) // page, T, "cuda")
+    new.K.fill_(float("nan")); new.V.fill_(float("nan"))
+    new.pack(src, extra=2 * T)
+    assert new.pages_free() == 0 and used * page < nl * B * Hkv * cap
+    room = cap + 2 * T
+    Kw, Vw = (np.zeros((nl, B, Hkv, room, 128)) for _ in range(2))
+    Kw[:, :, :, :cap], Vw[:, :, :, :cap] = want["Kc"].reshape(nl, B, Hkv, cap, 128), want["Vc"].reshape(nl, B, Hkv, cap, 128)
+    cs = L.rope_table(300)
+    base = np.array([100, 150, 70])
+    for step in range(2):
+        par = [[int(r.integers(-1, t)) if t else -1 for t in range(T)] for _ in range(B)]
+        mask = L.tree_mask(torch.tensor(par)).cuda()
+        see = np.zeros((B, T, T), bool)
+        depth = np.zeros((B, T), int)
+        for b in range(B):
+            for t in range(T):
+                if par[b][t] >= 0:
+                    see[b, t], depth[b, t] = see[b, par[b][t]], depth[b, par[b][t]] + 1
+                see[b, t, t] = True
+        count = np.array([T, 4, 7])
+        pos = base[:, None] + depth
+        last = [int(r.integers(0, c)) for c in count]                  # the leaf whose path is accepted
+        index, accepted = np.zeros((B, T), int), np.zeros(B, int)
+        for b in range(B):
+            path = np.flatnonzero(see[b, last[b]])
+            index[b, :len(path)], accepted[b] = path, len(path)
+        for l in range(nl):
+            q, k, v = bf(r, B, T, H, 128), bf(r, B, T, Hkv, 128), bf(r, B, T, Hkv, 128)
+            out = new.draft_layer(l, q.cuda(), k.cuda(), v.cuda(), dev(pos), cs, mask=mask, count=dev(count))
+            torch.cuda.synchronize()
+            qr, kr = f64(new.q), f64(new.Kd[l]).swapaxes(1, 2)
+            wq, wk = DO.rotate(f64(q), pos, cs.cpu().numpy()), DO.rotate(f64(k), pos, cs.cpu().numpy())
+            for b in range(B):
+                assert (np.abs(qr[b, :count[b]] - wq[b, :count[b]]) <= 2.0 ** -8 * np.abs(wq[b, :count[b]]) + 2.0 ** -20).all()
+                assert (np.abs(kr[b, :count[b]] - wk[b, :count[b]]) <= 2.0 ** -8 * np.abs(wk[b, :count[b]]) + 2.0 ** -20).all()
+            kd = np.nan_to_num(kr.swapaxes(1, 2))                     # what was rounded to bf16 is what is attended to
+            vd = f64(v).swapaxes(1, 2)
+            wo, _ = DO.tree_attn(qr, Kw[l], Vw[l], length[l], kd, vd, see, count)
+            tol, _ = tree_bound(np.nan_to_num(qr), np.concatenate([Kw[l], kd], 2), np.concatenate([Vw[l], vd], 2), room, 1 / np.sqrt(128))
+            for b in range(B):
+                assert (np.abs(f64(out)[b, :count[b]] - wo[b, :count[b]]) <= 2.0 ** -8 * np.abs(wo[b, :count[b]]) + tol).all()
+            Kw[l], Vw[l], length[l] = DO.commit(Kw[l], Vw[l], length[l], kd, vd, index, accepted)
+        new.commit(dev(index), dev(accepted))
+        base = base + accepted
+        assert new.status.item() == 0 and np.array_equal(i32(new.len), length)
+        for l in range(nl):
+            lg, lv = f64(logical(new.K, new.table[l].clamp_min(0))), f64(logical(new.V, new.table[l].clamp_min(0)))
+            for b in range(B):
+                for g in range(Hkv):
+                    m = length[l, b, g]
+                    assert np.array_equal(lg[b, g, :m], Kw[l, b, g, :m]) and np.array_equal(lv[b, g, :m], Vw[l, b, g, :m])
+    q = bf(r, B, 1, H, 128)
+    got, _ = L.tree_attn(q.cuda(), new.K, new.V, new.len[1], table=new.table[1])
+    want = O.decode_attn(f64(q)[:, 0], Kw[1], Vw[1], length[1])
+    tol, _ = tree_bound(f64(q), Kw[1], Vw[1], room, 1 / np.sqrt(128))
+    assert (np.abs(f64(got)[:, 0] - want["out"]) <= 2.0 ** -7 * np.abs(want["out"]) + tol).all()       # (the oracle's is rounded too)
+    with pytest.raises(RuntimeError):
+        new.reserve(new.len.cpu() + 4 * page)
+
+
+@pytest.mark.parametrize("H,Hkv,T,lens", [(8, 2, 3, [700, 33, 5, 129]), (8, 1, 30, [3000, 100]), (2, 2, 200, [300, 40, 0, 511])])
+def test_a_step_in_a_graph(H, Hkv, T, lens):
+    """Append, attention and commit captured once and replayed over caches that grow: as the same calls made one by one."""
+    B = len(lens) // Hkv
+    r = np.random.default_rng(T)
+    n_pages, page, mp = 60 * B * Hkv, 64, 60
+    tab = dev(r.permutation(n_pages).reshape(B, Hkv, mp))
+    K, V = bf(r, n_pages, page, 128).cuda(), bf(r, n_pages, page, 128).cuda()
+    cs = L.rope_table(500)
+    steps = [(bf(r, B, T, H + 2 * Hkv, 128).cuda(), dev(r.integers(0, 500, size=(B, T))), words_of(np.stack([random_tree(r, T, "tree")[0] for _ in range(B)])),
+              dev(r.integers(1, T + 1, size=B)), dev(np.sort(r.integers(0, T, size=(B, T)), axis=1))) for _ in range(3)]
+
+    def run(graph):
+        Kc, Vc, ln, st = K.clone(), V.clone(), dev(np.reshape(lens, (B, Hkv))), flag()
+        qkv, pos, mask, count, index = (x.clone() for x in steps[0])
+        Kd, Vd = (torch.zeros(B, Hkv, T, 128, dtype=BF, device="cuda") for _ in range(2))
+        qr, out, lse = torch.zeros(B, T, H, 128, dtype=BF, device="cuda"), torch.zeros(B, T, H, 128, dtype=BF, device="cuda"), torch.zeros(B, H, T, device="cuda")
+        ws = L.alloc_workspace(L.OP_TREE_ATTN, L.tree_dims(qr, Kc, tab, Kd), "cuda")
+
+        def step():
+            L.rope_append(qkv[:, :, H:H + Hkv], qkv[:, :, H + Hkv:], pos, cs, Kd, Vd, q=qkv[:, :, :H], q_out=qr, count=count, dev_status=st)
+            L.tree_attn(qr, Kc, Vc, ln, Kd=Kd, Vd=Vd, mask=mask, count=count, table=tab, out=out, lse=lse, ws=ws, dev_status=st)
+            L.commit_rows(Kd, Vd, Kc, Vc, ln, count, index=index, table=tab, dev_status=st)
+
+        if graph:
+            saved = Kc.clone(), Vc.clone(), ln.clone()
+            s = torch.cuda.Stream()
+            s.wait_stream(torch.cuda.current_stream())
+            with torch.cuda.stream(s):
+                step()
+            torch.cuda.current_stream().wait_stream(s)
+            torch.cuda.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                step()
+            for a, b in zip((Kc, Vc, ln), saved):
+                a.copy_(b)
+            for x in (qr, out, lse):
+                x.zero_()
+        got = []
+        for x in steps:
+            for a, b in zip((qkv, pos, mask, count, index), x):
+                a.copy_(b)
+            g.replay() if graph else step()
+            got += [t.clone() for t in (qr, out, lse, ln)]
+        torch.cuda.synchronize()
+        assert st.item() == 0
+        return got + [Kc, Vc]
+
+    for a, b in zip(run(False), run(True)):
+        assert torch.equal(a, b)
+
+
+def test_two_calls_at_once():
+    """Two streams, a workspace each: neither disturbs the other."""
+    r = np.random.default_rng(5)
+    problems = []
+    for B, H, Hkv, T, cap in ((2, 8, 2, 40, 3000), (1, 28, 4, 26, 3008)):
+        t = [x.cuda() for x in (bf(r, B, T, H, 128), bf(r, B, Hkv, cap, 128), bf(r, B, Hkv, cap, 128), bf(r, B, Hkv, T, 128), bf(r, B, Hkv, T, 128))]
+        ln = dev(r.integers(cap // 2, cap, size=(B, Hkv)))
+        ws = L.alloc_workspace(L.OP_TREE_ATTN, L.tree_dims(t[0], t[1], None, t[3]), "cuda")
+        alone, _ = L.tree_attn(*t[:3], ln, Kd=t[3], Vd=t[4], ws=ws)
+        problems.append((t, ln, ws, alone.clone(), torch.cuda.Stream(), torch.empty_like(alone)))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for t, ln, ws, _, s, out in problems:
+            L.tree_attn(*t[:3], ln, Kd=t[3], Vd=t[4], ws=ws, out=out, stream=s)
+    torch.cuda.synchronize()
+    for t, ln, ws, alone, s, out in problems:
+        assert same(out, alone)
