@@ -511,7 +511,7 @@ extern "C" lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void*
         const uint64_t strides[4] = {(uint64_t)a.q_sh * 2, (uint64_t)a.q_sn * 2, (uint64_t)a.G * a.q_sh * 2, (uint64_t)a.q_sb * 2};
         const uint32_t box[5] = {64, (uint32_t)a.G, (uint32_t)(kTreeTcRows / a.G), 1, 1};
         if (!make_tmap_bf16(&m.q, q, 5, dims, strides, box)) return LVLM_ERR_CUDA;
-        st = launch_tree_tc(a, m, (int)L.ctas, stream);
+        st = launch_tree_tc(a, m, stream);
     } else {
         return L.R == 1 ? launch_tree_mma<1>(a, m, L, stream) : launch_tree_mma<2>(a, m, L, stream);
     }

@@ -63,6 +63,6 @@ __device__ __forceinline__ uint32_t tree_see(const TreeArgs& a, int b, int t, in
 }
 
 struct TreeMaps { CUtensorMap q, k, v, kd, vd; };
-lvlm_status launch_tree_tc(const TreeArgs& a, const TreeMaps& m, int ctas, cudaStream_t stream);
+lvlm_status launch_tree_tc(const TreeArgs& a, const TreeMaps& m, cudaStream_t stream);
 
 }  // namespace lvlm

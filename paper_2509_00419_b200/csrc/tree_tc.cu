@@ -65,7 +65,7 @@ __device__ __forceinline__ bool tree_wait(uint64_t* bar, uint32_t parity, TreeTc
 __device__ __forceinline__ int tree_rt(const TreeHead& h, int tt) { return h.n <= tt ? (h.n > 0) : (h.n + tt - 1) / tt; }
 __device__ __forceinline__ int tree_weight(const TreeHead& h, int tt) { return max(h.nt, 1) * tree_rt(h, tt); }
 
-// RUNS: the grid shares out the key tiles of all units; else a CTA has one part of one unit, and no scheduler
+// RUNS: the grid shares out the key tiles of all units; else it is (unit, part, head), a CTA has one part of one unit, and no scheduler
 template <bool RUNS>
 __global__ void __launch_bounds__(kTThreads, 1)
 tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__ CUtensorMap kmap, const __grid_constant__ CUtensorMap vmap,
@@ -103,22 +103,11 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     const uint32_t tmem_base = __shfl_sync(0xFFFFFFFFu, sm->tmem_base, 0);
     pdl_enter();
 
-    const int G = a.G, T = a.T, Hkv = a.c.Hkv, heads = a.B * Hkv, tt = kTT / G, me = blockIdx.x;      // tt drafts a row tile
+    const int G = a.G, T = a.T, Hkv = a.c.Hkv, heads = a.B * Hkv, tt = kTT / G;      // tt drafts a row tile
+    const int me = RUNS ? blockIdx.x : (blockIdx.z * gridDim.y + blockIdx.y) * gridDim.x + blockIdx.x;
     const int pairs = a.units, ut = a.unit_tiles;
     long long total = 0, per = 0, lo = 0, hi = 0;
-    if (!RUNS) {
-        if (threadIdx.x == 0) {                                   // a part of a unit a CTA: one segment
-            const int pair = me % pairs, part = me / pairs % a.S, hd = me / pairs / a.S;
-            const TreeHead h = tree_head(a, hd, kTT);
-            const int step = tree_part(h, a.S), t0 = part * step, rt = tree_rt(h, tt);
-            TreeSeg w;
-            w.hd = ut * pair < rt && (t0 < h.nt || part == 0) ? hd : -1;
-            w.tile = ut * pair; w.t0 = t0; w.nk = min(h.nt - t0, step); w.split = ut == 1 || ut * pair + 1 == rt; w.n = h.n; w.ln = h.ln;
-            w.slot = step >= h.nt ? -1 : me;
-            sm->seg[0] = w;
-        }
-        __syncthreads();
-    } else {
+    if (RUNS) {
     // ---- my run [lo, hi) of the weights of all heads, and the head it begins in ------------------------------------
     const int each = (heads + kTThreads - 1) / kTThreads, h_lo = min(heads, (int)threadIdx.x * each), h_hi = min(heads, h_lo + each);
     long long sum = 0;
@@ -164,7 +153,6 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
     }
     // the s-th segment of my run has been laid out: false where there is none
     auto segment = [&](int s) -> bool {
-        if (!RUNS) return s == 0 && sm->seg[0].hd >= 0;
         if (!__all_sync(0xFFFFFFFFu, tree_wait(&sm->seg_full[s % kTSegs], (s / kTSegs) & 1, sm, a))) return false;
         return sm->seg[s % kTSegs].hd >= 0;
     };
@@ -181,12 +169,39 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         const int box_rows = a.c.page ? min(a.c.page, kTT) : kTT, boxes = kTT / box_rows;
         const int half = lane & 1, x = lane >> 1;
         int kc = 0, qc = 0;                                       // tiles and query tiles fetched for the segments before
+        auto load_q = [&](int b, int g, int tile, int nq) {
+            mbar_arrive_expect_tx(&sm->q_full, (uint32_t)(nq * 2 * tt * G * 128));
+            for (int u = 0; u < nq; ++u) {
+                tma_load_5d(sQ + u * kTTile, &qmap, &sm->q_full, 0, 0, (tile + u) * tt, g, b);
+                tma_load_5d(sQ + u * kTTile + kTHalf, &qmap, &sm->q_full, 64, 0, (tile + u) * tt, g, b);
+            }
+        };
         bool ok = true;
 #pragma unroll 1
         for (int s = 0; ok && (RUNS || s == 0); ++s) {
-            if (!segment(s)) break;
-            const TreeSeg w = sm->seg[s % kTSegs];
-            segment_done(s);
+            TreeSeg w;
+            if (RUNS) {
+                if (!segment(s)) break;
+                w = sm->seg[s % kTSegs];
+                segment_done(s);
+            } else {
+                // a part of a unit a CTA, its one segment, worked out here; the queries do not wait for the length
+                const int pair = blockIdx.x, part = blockIdx.y, hd = blockIdx.z;
+                if (lane == 0) load_q(hd / Hkv, hd % Hkv, ut * pair, ut);
+                const TreeHead h = tree_head(a, hd, kTT);
+                const int step = tree_part(h, a.S), t0 = part * step, rt = tree_rt(h, tt);
+                w.hd = ut * pair < rt && (t0 < h.nt || part == 0) ? hd : -1;
+                w.tile = ut * pair; w.t0 = t0; w.nk = min(h.nt - t0, step); w.split = ut == 1 || ut * pair + 1 == rt; w.n = h.n; w.ln = h.ln;
+                w.slot = step >= h.nt ? -1 : me;
+                if (lane == 0) {
+                    sm->seg[0] = w;
+                    mbar_arrive(&sm->seg_full[0]);
+                }
+                if (w.hd < 0 || w.nk == 0) {                      // nobody else waits for the queries, and no copy outlives its CTA
+                    tree_wait(&sm->q_full, 0, sm, a);
+                    break;
+                }
+            }
             const int b = w.hd / Hkv, g = w.hd % Hkv, ns = w.ln > 0 ? (w.ln + kTT - 1) / kTT : 0;
             // the page of my box of tile t; entries behind the head's length are not read: its last page again
             auto page_of = [&](int t) -> int {
@@ -196,20 +211,13 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
             };
             int id = page_of(w.t0), id_next = w.nk > 1 ? page_of(w.t0 + 1) : 0;      // asked for two tiles ahead
             // the queries: behind the first keys, once the epilogue of the segment before has left their place
-            const int q_at = w.nk == 0 ? -1 : qc == 0 ? 0 : min(kTStages, w.nk);
+            const int q_at = w.nk == 0 || !RUNS ? -1 : qc == 0 ? 0 : min(kTStages, w.nk);
 #pragma unroll 1
             for (int j = 0; j <= w.nk; ++j) {
                 if (j == q_at) {
                     ok = qc == 0 || __all_sync(0xFFFFFFFFu, tree_wait(&sm->e_done, (qc - 1) & 1, sm, a));
                     if (!ok) break;
-                    if (lane == 0) {
-                        const int nq = w.split ? 1 : 2;
-                        mbar_arrive_expect_tx(&sm->q_full, (uint32_t)(nq * 2 * tt * G * 128));
-                        for (int u = 0; u < nq; ++u) {
-                            tma_load_5d(sQ + u * kTTile, &qmap, &sm->q_full, 0, 0, (w.tile + u) * tt, g, b);
-                            tma_load_5d(sQ + u * kTTile + kTHalf, &qmap, &sm->q_full, 64, 0, (w.tile + u) * tt, g, b);
-                        }
-                    }
+                    if (lane == 0) load_q(b, g, w.tile, w.split ? 1 : 2);
                     ++qc;
                 }
                 if (j == w.nk) break;
@@ -574,7 +582,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
 }
 
 template <bool RUNS>
-static lvlm_status launch_tree_tc(const TreeArgs& a, const TreeMaps& m, int ctas, cudaStream_t stream) {
+static lvlm_status launch_tree_tc(const TreeArgs& a, const TreeMaps& m, dim3 ctas, cudaStream_t stream) {
     const size_t smem = 1024 + (size_t)kTTile * (2 + 2 * kTStages) + sizeof(TreeTcSmem);
     LVLM_RETURN_IF_CUDA(cudaFuncSetAttribute(tree_tc_kernel<RUNS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
     static const int regs = [] {
@@ -582,11 +590,12 @@ static lvlm_status launch_tree_tc(const TreeArgs& a, const TreeMaps& m, int ctas
         return cudaFuncGetAttributes(&f, tree_tc_kernel<RUNS>) == cudaSuccess ? f.numRegs : 0;
     }();
     if (3 * regs < kTRegsFew + 2 * kTRegsMany) return LVLM_ERR_CUDA;       // the split would wait for registers that nobody has
-    return launch_kernel(tree_tc_kernel<RUNS>, dim3((unsigned)ctas), dim3(kTThreads), smem, stream, 1, m.q, m.k, m.v, m.kd, m.vd, a);
+    return launch_kernel(tree_tc_kernel<RUNS>, ctas, dim3(kTThreads), smem, stream, 1, m.q, m.k, m.v, m.kd, m.vd, a);
 }
 
-lvlm_status launch_tree_tc(const TreeArgs& a, const TreeMaps& m, int ctas, cudaStream_t stream) {
-    return a.runs ? launch_tree_tc<true>(a, m, ctas, stream) : launch_tree_tc<false>(a, m, ctas, stream);
+lvlm_status launch_tree_tc(const TreeArgs& a, const TreeMaps& m, cudaStream_t stream) {
+    if (a.runs) return launch_tree_tc<true>(a, m, dim3(kTreeTcCtas), stream);
+    return launch_tree_tc<false>(a, m, dim3((unsigned)a.units, (unsigned)a.S, (unsigned)(a.B * a.c.Hkv)), stream);     // (148 CTAs at most)
 }
 
 }  // namespace lvlm
