@@ -305,16 +305,19 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
     cluster_wait();                                             // and nobody leaves while its own is still read
 }
 
-// Adds the parts of a unit that was cut, in order.  Lane = row, a warp CH groups of four
-// channels of 32 rows: the loads are the lines that the parts were stored in.  grid (units, row blocks, channel blocks).
-// Bound by latency where parts are many: lengths are read before the wait for the kernel ahead (it has waited for whatever wrote
-// them), the first outputs are on their way while the weights are worked out, which the warps share.
+// Adds the parts of a unit that was cut.  Lane = row, a warp CH groups of four channels of 32 rows: the loads are the lines that the parts
+// were stored in.  SL warps share the same channels: each takes every SL-th part, and they are added in their order.  grid (units, row
+// blocks, channel blocks).  Bound by latency where parts are many and units few: lengths are read before the wait for the kernel ahead
+// (it has waited for whatever wrote them), the first outputs are on their way while the weights are worked out, which the warps share.
+// 4 units of 37 parts: 9.5 us with a warp going through all parts, 4.8 with four.
 constexpr int kTreeCombineWarps = 8;
 constexpr int kTreeMostParts = kTreeTcCtas;
-template <int CH>
+template <int CH, int SL>
 __global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(const TreeArgs a) {
     __shared__ float s_m[kTreeMostParts][32], s_l[kTreeMostParts][32];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    __shared__ float4 s_v[SL > 1 ? kTreeCombineWarps : 1][32];
+    __shared__ float s_ls[SL > 1 ? kTreeCombineWarps : 1][32];
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slice = warp % SL;
     const int hd = blockIdx.x / a.units, unit = blockIdx.x % a.units, b = hd / a.c.Hkv, g = hd % a.c.Hkv;
     const int place = blockIdx.y * 32 + lane, row = place % kTreeTcRows, tile = unit * a.unit_tiles + place / kTreeTcRows;
     const TreeHead h = tree_head(a, hd, kTreeTcRows);
@@ -333,22 +336,22 @@ __global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(co
     if (of.x < 0) return;                                       // not cut
     const int r = tile * a.tile_rows + row, t = r / a.G;
     const bool mine = row < a.tile_rows && t < h.n;
-    const int c0 = (blockIdx.z * kTreeCombineWarps + warp) * CH, parts = min(of.y + 1, kTreeMostParts);
+    const int c0 = (blockIdx.z * (kTreeCombineWarps / SL) + warp / SL) * CH, parts = min(of.y + 1, kTreeMostParts);
     // (runs: part p >= 1 lies in the first slot of its CTA)
     const int rest = a.runs ? of.x & ~1 : of.x;
     auto slot = [&](int p) -> int64_t { return p == 0 ? of.x : rest + stride * p; };
     constexpr int kAhead = 16 / CH;
     float4 x[kAhead][CH];
-    auto fetch = [&](int p0) {
+    auto fetch = [&](int p0) {                                  // parts p0, p0 + SL, ...
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
-            if (p0 + u < parts) {
-                const float4* from = reinterpret_cast<const float4*>(a.part_o + slot(p0 + u) * a.pitch * kHeadDim) + place;
+            if (p0 + u * SL < parts) {
+                const float4* from = reinterpret_cast<const float4*>(a.part_o + slot(p0 + u * SL) * a.pitch * kHeadDim) + place;
 #pragma unroll
                 for (int c = 0; c < CH; ++c) x[u][c] = from[(c0 + c) * a.pitch];
             }
     };
-    fetch(0);
+    fetch(slice);
     for (int p = warp; p < parts; p += kTreeCombineWarps) {
         const float2 ml = a.part_ml[slot(p) * a.pitch + place];
         s_m[p][lane] = ml.x;
@@ -356,24 +359,37 @@ __global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(co
     }
     __syncthreads();
     float M = -INFINITY, Ls = 0.f;
+#pragma unroll 8
     for (int p = 0; p < parts; ++p) M = fmaxf(M, s_m[p][lane]);
     float4 v[CH];
 #pragma unroll
     for (int c = 0; c < CH; ++c) v[c] = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int p0 = 0;;) {
+    for (int p0 = slice; p0 < parts;) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            if (p0 + u >= parts) break;
-            const float m = s_m[p0 + u][lane];
+            const int p = p0 + u * SL;
+            if (p >= parts) break;
+            const float m = s_m[p][lane];
             if (m == -INFINITY) continue;                       // (without weight)
             const float w = ex2_fast(m - M);
-            Ls += s_l[p0 + u][lane] * w;
+            Ls += s_l[p][lane] * w;
 #pragma unroll
             for (int c = 0; c < CH; ++c) { v[c].x += x[u][c].x * w; v[c].y += x[u][c].y * w; v[c].z += x[u][c].z * w; v[c].w += x[u][c].w * w; }
         }
-        p0 += kAhead;
-        if (p0 >= parts) break;
-        fetch(p0);
+        p0 += kAhead * SL;
+        if (p0 < parts) fetch(p0);
+    }
+    if (SL > 1) {
+        s_v[warp][lane] = v[0];
+        s_ls[warp][lane] = Ls;
+        __syncthreads();
+        if (slice > 0) return;
+#pragma unroll
+        for (int w = 1; w < SL; ++w) {
+            const float4 y = s_v[warp + w][lane];
+            v[0].x += y.x; v[0].y += y.y; v[0].z += y.z; v[0].w += y.w;
+            Ls += s_ls[warp + w][lane];
+        }
     }
     if (!mine) return;
     const int head = g * a.G + r % a.G;
@@ -516,10 +532,12 @@ extern "C" lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void*
         return L.R == 1 ? launch_tree_mma<1>(a, m, L, stream) : launch_tree_mma<2>(a, m, L, stream);
     }
     if (st != LVLM_OK || (L.S == 1 && !L.runs)) return st;
-    // a warp takes one group of channels where few units leave the GPU idle otherwise
+    // the fewer units, the finer.  us of the whole call with <1, 4> / <1, 1> / <4, 1>: 4 units of 37 parts 26.7 / 31.4 / 50, 8 of 12 18.8 /
+    // 16.1 / 16.9, 16 of 9 - / 23.5 / 22.4, 32 of 2 29.5 / 16.9 / 14.1
     const int64_t units = (int64_t)d->B * d->Hkv * L.units;
     const unsigned blocks = (unsigned)(L.pitch / 32);
-    if (units * blocks < kTreeTcCtas)
-        return launch_kernel(tree_combine_kernel<1>, dim3((unsigned)units, blocks, 4), dim3(kTreeCombineWarps * 32), 0, stream, 1, a);
-    return launch_kernel(tree_combine_kernel<4>, dim3((unsigned)units, blocks, 1), dim3(kTreeCombineWarps * 32), 0, stream, 1, a);
+    const dim3 threads(kTreeCombineWarps * 32);
+    if (units * blocks * 16 <= 2 * kTreeTcCtas) return launch_kernel(tree_combine_kernel<1, 4>, dim3((unsigned)units, blocks, 16), threads, 0, stream, 1, a);
+    if (units * blocks * 4 <= kTreeTcCtas) return launch_kernel(tree_combine_kernel<1, 1>, dim3((unsigned)units, blocks, 4), threads, 0, stream, 1, a);
+    return launch_kernel(tree_combine_kernel<4, 1>, dim3((unsigned)units, blocks, 1), threads, 0, stream, 1, a);
 }
