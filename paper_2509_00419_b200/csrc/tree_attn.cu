@@ -425,22 +425,27 @@ static bool tree_layout(const lvlm_dims* d, int64_t cap, TreeLayout* L) {
     const int64_t tc_steps = (keys + kTreeTcRows - 1) / kTreeTcRows + (drafts + kTreeTcRows - 1) / kTreeTcRows;
     const int unit_tiles = tree_unit_tiles(heads, tiles, keys), tc_units = (tiles + unit_tiles - 1) / unit_tiles;
     const int64_t units = heads * tc_units;
-    L->runs = units > kTreeTcCtas;
-    int64_t parts = L->runs ? 1 : kTreeTcCtas / units;
+    int64_t parts = units < kTreeTcCtas ? kTreeTcCtas / units : 1;
     const int64_t most = tc_steps / 2;                       // (two key tiles or more a part: one, and more parts, is no faster)
     parts = parts > most ? (most > 0 ? most : 1) : parts;
+    // More units than SMs: a CTA each, in waves, or runs.  Estimates of either in us, for equal lengths (us measured, waves / runs): 256 units of
+    // two row tiles, 216 keys 40 / 52, 1100 72 / 85, 3008 153 / 164, 9000 440 / 479; 160 of one, 1100 keys 46 / 53, 9000 232 / 151; 224
+    // of two, 3008 keys 150 / 143, 16640 700 / 577.
+    const double turn = unit_tiles == 2 ? 2.85 : 1.45, waves_us = (double)((units + kTreeTcCtas - 1) / kTreeTcCtas) * ((double)(tc_steps + parts - 1) / parts * turn + 7);
+    const double runs_us = 30 + 1.15 * 1.43 * (double)heads * tiles * tc_steps / kTreeTcCtas;
+    L->runs = (units > kTreeTcCtas && runs_us < waves_us) || heads > 65535;
     // mma.sync
     const int R = (rows + kTreeRows - 1) / kTreeRows, room = R == 1 ? 2 * kTreeTcCtas : kTreeTcCtas;       // CTAs that run at a time
     const int64_t stages = (keys + kTreeStageKeys - 1) / kTreeStageKeys + (drafts + kTreeStageKeys - 1) / kTreeStageKeys;
     int S = 1;
     while (S < kTreeMaxCluster && heads * 2 * S <= room && stages >= 2 * S) S *= 2;
 
-    // Estimates of either in us, fitted to caches of 100 to 33000 keys of 4 to 256 heads (10 % off): a stage a CTA of the one, a key tile a
-    // CTA of the other.  Measured, mma.sync / tcgen05: 16 rows or less, 4 heads x 3008 keys 10.8 / 13.0, x 9000 22 / 17; 16 heads x 9000
-    // 26 / 26; 64 heads x 9000 51 / 68; 17 to 32 rows, 8 heads x 1100 10.2 / 11.5, x 9000 27 / 20, 64 heads x 3008 35 / 33.
+    // Estimates in us, fitted to caches of 100 to 33000 keys of 4 to 256 heads (10 % off), from a stage a CTA.  Measured, mma.sync / tcgen05:
+    // 16 rows or less, 4 heads x 3008 keys 10.8 / 13.0, x 9000 22 / 17; 16 heads x 9000 26 / 26; 64 heads x 9000 51 / 68; 17 to 32 rows,
+    // 8 heads x 1100 10.2 / 11.5, x 9000 27 / 20, 64 heads x 3008 35 / 33.
     const int64_t waves = (heads * S + room - 1) / room, run = (stages + S - 1) / S;
     const double mma_us = R == 1 ? 5 + (heads * S <= kTreeTcCtas ? 1.0 : 1.2) * waves * run : 7 + 1.13 * waves * run;
-    const double tc_us = 12 + 1.55 * (L->runs ? (double)heads * tiles * tc_steps / kTreeTcCtas : (double)((tc_steps + parts - 1) / parts) * unit_tiles);
+    const double tc_us = units <= kTreeTcCtas ? 12 + 1.55 * (double)((tc_steps + parts - 1) / parts) * unit_tiles : L->runs ? runs_us : waves_us;
     L->tc = R > 2 || d->T > 32 * kTreeMmaWords || tc_us < mma_us;
     L->R = R;
     L->S = L->tc ? (int)parts : S;

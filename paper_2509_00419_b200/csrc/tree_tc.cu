@@ -7,10 +7,11 @@
 //   softmax          thread = query row, running maximum and sum in the log2 domain; probabilities go back as bf16 head + bf16
 //                    remainder over the logits they came from (a plain bf16 would cost as much again as the rounding of the result)
 //   O += P V_j       A = P from tensor memory, B = V as it lies in memory
-// One CTA an SM.  With fewer units than SMs a unit is cut into equal parts, a CTA each.  With more (a.runs), lengths being ragged and only
-// known on the device, the key tiles of all units, weighted by what they take, are laid end to end there and every CTA takes an
-// equal run of them: a scheduler warp cuts the run into segments, a unit each, and the other warps work through them without
-// stopping in between (the keys of the next segment are fetched during the epilogue of this one).
+// One CTA an SM.  With fewer units than SMs a unit is cut into equal parts, a CTA each.  With more, a unit is a CTA's, in waves; or, where
+// long units would leave the last wave half empty (a.runs), the key tiles of all units, weighted by what they take, are laid end to end
+// - on the device, which alone knows the lengths - and every CTA takes an equal run of them: a scheduler warp cuts the run into segments,
+// a unit each, and the other warps work through them without stopping in between (the keys of the next segment are fetched during
+// the epilogue of this one).
 // A unit that is cut leaves its parts (max, sum, output) in the workspace; tree_combine_kernel adds them in order.
 // Rows of V behind the end of the cache or of the drafts are zeroed in shared memory before they are multiplied: they may hold
 // anything, and their weight of zero would not stop a NaN.
@@ -595,7 +596,7 @@ static lvlm_status launch_tree_tc(const TreeArgs& a, const TreeMaps& m, dim3 cta
 
 lvlm_status launch_tree_tc(const TreeArgs& a, const TreeMaps& m, cudaStream_t stream) {
     if (a.runs) return launch_tree_tc<true>(a, m, dim3(kTreeTcCtas), stream);
-    return launch_tree_tc<false>(a, m, dim3((unsigned)a.units, (unsigned)a.S, (unsigned)(a.B * a.c.Hkv)), stream);     // (148 CTAs at most)
+    return launch_tree_tc<false>(a, m, dim3((unsigned)a.units, (unsigned)a.S, (unsigned)(a.B * a.c.Hkv)), stream);
 }
 
 }  // namespace lvlm

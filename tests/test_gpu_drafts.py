@@ -277,7 +277,8 @@ def words_of(see):
     return dev(np.packbits(pad, axis=-1, bitorder="little").view(np.uint32).reshape(*see.shape[:-1], W).astype(np.int64).astype(np.uint32).view(np.int32))
 
 
-def run_tree(B, H, Hkv, T, lens, count, page, kind, seed, max_len=None, shared=False, fill=float("nan"), drafts=True, spread=1.0, cap=None):
+def run_tree(B, H, Hkv, T, lens, count, page, kind, seed, max_len=None, shared=False, fill=float("nan"), drafts=True, spread=1.0, cap=None,
+             entries=0):
     r = np.random.default_rng(seed)
     lens = np.asarray(lens).reshape(B, Hkv)
     unit = page or 1
@@ -298,6 +299,8 @@ def run_tree(B, H, Hkv, T, lens, count, page, kind, seed, max_len=None, shared=F
         for g in range(Hkv):
             K[b, g, lens[b, g]:], V[b, g, lens[b, g]:] = fill, fill
     Kc, Vc, tab = paged(r, K, V, page, fill) if page else (K.cuda(), V.cuda(), None)
+    if entries:                                                       # a longer table, its entries behind the pages never read
+        tab = torch.cat([tab, torch.full((B, Hkv, entries), -1, dtype=torch.int32, device="cuda")], 2).contiguous()
     mask = None if kind == "chain" or not drafts else words_of(see[0] if shared else see)
     o = torch.full((B, T, H, 128), 9.0, dtype=BF, device="cuda")
     ls = torch.full((B, H, T), 9.0, device="cuda")
@@ -351,6 +354,19 @@ def test_tree_attn_ragged_over_the_gpu(B, H, Hkv, T, page, seed):
     count = np.where(r.random(B) < 0.2, 0, r.integers(1, T + 1, size=B))
     count[0] = T
     run_tree(B, H, Hkv, T, lens.reshape(-1).tolist(), count.tolist(), page, "any", seed=seed)
+
+
+@pytest.mark.parametrize("B,H,Hkv,T,page,seed", [(20, 32, 8, 13, 64, 1), (13, 28, 4, 40, 128, 2), (10, 48, 8, 44, 16, 3), (160, 1, 1, 3, 32, 4)])
+def test_tree_attn_in_runs(B, H, Hkv, T, page, seed):
+    """More units than SMs and caches that may be long: every CTA takes an equal run of all key tiles, and units are cut anywhere."""
+    r = np.random.default_rng(seed)
+    lens = r.integers(0, 600, size=(B, Hkv))
+    lens[r.random((B, Hkv)) < 0.2] = 0
+    far = r.random((B, Hkv)) < 0.12
+    lens[far] = r.integers(1500, 3500, size=int(far.sum()))
+    count = np.where(r.random(B) < 0.2, 0, r.integers(1, T + 1, size=B))
+    count[0] = T
+    run_tree(B, H, Hkv, T, lens.reshape(-1).tolist(), count.tolist(), page, "any", seed=seed, entries=20000 // page)
 
 
 @pytest.mark.parametrize("max_len", [None, 1, 100, 3001, 100000])
