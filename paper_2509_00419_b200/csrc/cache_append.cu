@@ -24,7 +24,8 @@ struct RopeArgs {
     __nv_bfloat16* q_out; __nv_bfloat16* Kc; __nv_bfloat16* Vc;
     const int32_t* table; const int32_t* len; int32_t* len_out;
     float* acc_score; int32_t* pos_cache;
-    int B, H, T, rot, interleaved, n_pos, axes, sect0, sect1, bump;
+    int B, H, T, rot, interleaved, n_pos, axes, sect0, sect1;
+    int bump;                                      // 1: len_out is written (it is not len), 2: at the end (a sequence has one CTA)
     int64_t q_sb, q_sn, q_sh, qo_sb, qo_sn, qo_sh, n_sb, n_sn, n_sh;
     CacheGeom c;
     int32_t* dev_status;
@@ -138,7 +139,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == kRopeMany ? 18 : 1) rope_a
                 const int g = r - a.H - (key ? 0 : Hkv);
                 const int64_t hd = (int64_t)b * Hkv + g;
                 const int ln = checked_start(a.len, hd, n, a.c.cap, a.dev_status);
-                if (a.bump && key && t == 0 && lane8 == 0) a.len_out[hd] = ln >= 0 ? ln + n : a.len ? a.len[hd] : 0;
+                if (a.bump == 1 && key && t == 0 && lane8 == 0) a.len_out[hd] = ln >= 0 ? ln + n : a.len ? a.len[hd] : 0;
                 if (ln < 0 || !live) continue;
                 const int64_t off = cache_row(a.c, a.table, b, g, ln + t);
                 if (off < 0) { flag_bounds(a.dev_status); continue; }
@@ -162,6 +163,14 @@ __global__ void __launch_bounds__(THREADS, THREADS == kRopeMany ? 18 : 1) rope_a
             }
             reinterpret_cast<uint4*>(to[u])[c0] = x[u];
             reinterpret_cast<uint4*>(to[u])[c1] = y[u];
+        }
+    }
+    if (a.bump == 2) {                             // len_out is len, which every thread has read by now
+        __syncthreads();
+        for (int g = threadIdx.x; g < Hkv; g += THREADS) {
+            const int64_t hd = (int64_t)b * Hkv + g;
+            const int ln = checked_start(a.len, hd, n, a.c.cap, nullptr);
+            if (ln >= 0) a.len_out[hd] = ln + n;
         }
     }
 }
@@ -284,11 +293,11 @@ extern "C" lvlm_status lvlm_rope_append(const void* q, const void* k_new, const 
     a.table = table; a.len = len; a.len_out = len_out; a.acc_score = acc_score; a.pos_cache = pos_cache;
     a.rot = d->rot; a.interleaved = d->interleaved != 0; a.n_pos = d->n_pos; a.axes = axes; a.sect0 = d->sect0; a.sect1 = d->sect1;
     const bool in_place = len_out != nullptr && len_out == len;
-    a.bump = len_out != nullptr && !in_place;
+    a.bump = !len_out ? 0 : !in_place ? 1 : d->T == 1 ? 2 : 0;
     a.dev_status = dev_status;
     const lvlm_status st = tokens <= kRopeFewTokens ? launch_kernel(rope_append_kernel<kRopeFew>, dim3((unsigned)tokens), dim3(kRopeFew), 0, stream, 1, a)
                                                     : launch_kernel(rope_append_kernel<kRopeMany>, dim3((unsigned)tokens), dim3(kRopeMany), 0, stream, 1, a);
-    if (st != LVLM_OK || !in_place) return st;
+    if (st != LVLM_OK || !in_place || d->T == 1) return st;
     return grow_len(len_out, count, 0, (int)heads, a.c, d->T, stream);
 }
 

@@ -104,7 +104,7 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
             return a.table[(int64_t)hd * a.c.max_pages + (min(st * kTreeStageKeys + bx * box_rows, ln - 1) >> a.c.shift)];
         };
         int id = page_of(t_lo);
-        for (int i = 0; i < nstage; ++i) {
+        for (int i = 0; i < nstage && !tree_starved(a); ++i) {
             const int s = i % kStages, st = t_lo + i;
             const int id_next = i + 1 < nstage ? page_of(st + 1) : 0;      // asked for a stage ahead
             if (i >= kStages && !__all_sync(0xFFFFFFFFu, wait_on(&s_empty[s], (uint32_t)(i / kStages - 1) & 1u))) break;
@@ -472,7 +472,15 @@ size_t tree_attn_workspace(const lvlm_dims* d) {
     return tree_layout(d, cap, &L) ? L.total : 0;
 }
 
+#ifdef LVLM_TEST_HOOKS
+static int g_tree_starve = 0;
+#endif
+
 }  // namespace lvlm
+
+#ifdef LVLM_TEST_HOOKS
+extern "C" void lvlm_debug_starve_tree(int on) { lvlm::g_tree_starve = on ? 1 : 0; }
+#endif
 
 extern "C" lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void* Vc, const int32_t* table, const int32_t* len,
                                        const void* Kd, const void* Vd, const uint32_t* mask, const int32_t* count,
@@ -525,6 +533,9 @@ extern "C" lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void*
     a.part_o = reinterpret_cast<float*>(wsb + L.off_o);
     a.part_of = reinterpret_cast<int2*>(wsb + L.off_of);
     a.dev_status = dev_status;
+#ifdef LVLM_TEST_HOOKS
+    a.starve = g_tree_starve;
+#endif
     if (L.ctas > 0x7FFFFFFFll) return LVLM_ERR_UNSUPPORTED;
     lvlm_status st;
     if (L.tc) {

@@ -32,7 +32,17 @@ struct TreeArgs {
     int2* part_of;
     CacheGeom c;
     int32_t* dev_status;
+#ifdef LVLM_TEST_HOOKS
+    int starve;
+#endif
 };
+
+// The test build can keep the producers from fetching keys, so that waits run out.
+#ifdef LVLM_TEST_HOOKS
+__device__ __forceinline__ bool tree_starved(const TreeArgs& a) { return a.starve != 0; }
+#else
+__device__ __forceinline__ bool tree_starved(const TreeArgs&) { return false; }
+#endif
 
 __device__ __forceinline__ void tree_flag(const TreeArgs& a, int bit) {
     if (a.dev_status) atomicOr(a.dev_status, bit);

@@ -214,7 +214,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
             // the queries: behind the first keys, once the epilogue of the segment before has left their place
             const int q_at = w.nk == 0 || !RUNS ? -1 : qc == 0 ? 0 : min(kTStages, w.nk);
 #pragma unroll 1
-            for (int j = 0; j <= w.nk; ++j) {
+            for (int j = 0; j <= w.nk && !tree_starved(a); ++j) {
                 if (j == q_at) {
                     ok = qc == 0 || __all_sync(0xFFFFFFFFu, tree_wait(&sm->e_done, (qc - 1) & 1, sm, a));
                     if (!ok) break;
@@ -586,10 +586,12 @@ template <bool RUNS>
 static lvlm_status launch_tree_tc(const TreeArgs& a, const TreeMaps& m, dim3 ctas, cudaStream_t stream) {
     const size_t smem = 1024 + (size_t)kTTile * (2 + 2 * kTStages) + sizeof(TreeTcSmem);
     LVLM_RETURN_IF_CUDA(cudaFuncSetAttribute(tree_tc_kernel<RUNS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    static const int regs = [] {
+    static int regs = 0;                                                   // (looked up once; any thread finds the same)
+    if (regs == 0) {
         cudaFuncAttributes f;
-        return cudaFuncGetAttributes(&f, tree_tc_kernel<RUNS>) == cudaSuccess ? f.numRegs : 0;
-    }();
+        LVLM_RETURN_IF_CUDA(cudaFuncGetAttributes(&f, tree_tc_kernel<RUNS>));
+        regs = f.numRegs;
+    }
     if (3 * regs < kTRegsFew + 2 * kTRegsMany) return LVLM_ERR_CUDA;       // the split would wait for registers that nobody has
     return launch_kernel(tree_tc_kernel<RUNS>, ctas, dim3(kTThreads), smem, stream, 1, m.q, m.k, m.v, m.kd, m.vd, a);
 }

@@ -3,8 +3,10 @@ import numpy as np
 import pytest
 import torch
 
+from bench import count_launches
 from oracle import draft_oracle as DO
 from paper_2509_00419_b200 import binding as L
+from paper_2509_00419_b200 import build as BU
 from tests.util import f64, i32
 
 pytestmark = pytest.mark.gpu
@@ -384,10 +386,11 @@ def test_tree_attn_shared_mask_large_logits_no_drafts():
     run_tree(2, 8, 2, 12, [50, 9, 70, 100], [12, 5], 64, "any", seed=3, fill=float("inf"))
 
 
-def test_tree_attn_flags():
+@pytest.mark.parametrize("T", [3, 60])
+def test_tree_attn_flags(T):
     """A bad length, count or page number: flagged, nothing outside is read, the other heads are as without it."""
     r = np.random.default_rng(12)
-    B, H, Hkv, T, page = 2, 4, 2, 3, 16
+    B, H, Hkv, page = 2, 4, 2, 16
     K, V, Kd, Vd, q = bf(r, B, Hkv, 48, 128), bf(r, B, Hkv, 48, 128), bf(r, B, Hkv, T, 128), bf(r, B, Hkv, T, 128), bf(r, B, T, H, 128)
     Kp, Vp, tab = paged(r, K, V, page, fill=0.0)
 
@@ -405,7 +408,7 @@ def test_tree_attn_flags():
         s, o, l = go(ln=((40, 20), (bad, 7)))
         assert s == L.DEV_BOUNDS and (o[1, :, :2] == 0).all() and torch.isneginf(l[1, :2]).all()
         assert same(o[0], o0[0]) and same(o[1, :, 2:], o0[1, :, 2:])
-    for bad in (-1, 4):
+    for bad in (-1, T + 1):
         s, o, _ = go(count=(T, bad))
         assert s == L.DEV_BOUNDS and (o[1] == 9).all() and same(o[0], o0[0])
     zeroed = K.clone(), V.clone()
@@ -413,7 +416,7 @@ def test_tree_attn_flags():
         x[0, 1, :16] = 0                                             # the page's rows are taken as zeros
     see = np.tril(np.ones((T, T), bool))[None].repeat(B, 0)
     want, _ = DO.tree_attn(f64(q), f64(zeroed[0]), f64(zeroed[1]), np.array([[40, 20], [33, 7]]), f64(Kd), f64(Vd), see, [T, T])
-    tol, _ = tree_bound(f64(q), f64(K), f64(V), 51, 1 / np.sqrt(128))
+    tol, _ = tree_bound(f64(q), f64(K), f64(V), 48 + T, 1 / np.sqrt(128))
     for bad in (-1, Kp.shape[0], 1 << 30, -(1 << 31)):
         s, o, _ = go(broken=bad)
         assert s == L.DEV_BOUNDS and same(o[1], o0[1]) and same(o[0, :, :2], o0[0, :, :2])
@@ -619,3 +622,100 @@ def test_two_calls_at_once():
     torch.cuda.synchronize()
     for t, ln, ws, alone, s, out in problems:
         assert same(out, alone)
+
+
+# ---- forms, workspaces, waits ----------------------------------------------------------------------------------------
+FORMS = [  # B, H, Hkv, T, rows, expected rows, launches
+    (1, 28, 4, 1, 300, None, 1), (2, 32, 8, 8, 400, None, 1),          # mma.sync, clusters
+    (1, 28, 4, 20, 100, None, 1), (1, 28, 4, 20, 1500, None, 2),       # tcgen05: a part a unit; parts, which a second launch adds
+    (1, 28, 4, 1, 300, 30000, 2), (60, 32, 8, 13, 60, None, 1),        # long caches expected; units in waves
+    (20, 32, 8, 13, 200, 9000, 2)]                                     # in runs
+
+
+def _form(B, H, Hkv, T, rows, expected, paged_to=0):
+    g = torch.Generator(device="cuda").manual_seed(rows + T)
+    bfg = lambda *s: torch.randn(*s, generator=g, device="cuda").bfloat16()
+    q, Kd, Vd = bfg(B, T, H, 128), bfg(B, Hkv, T, 128), bfg(B, Hkv, T, 128)
+    page, mp = 64, max(rows, expected or 0) // 64 + 1
+    used = rows // page + 1
+    Kp, Vp = bfg(B * Hkv * used, page, 128), bfg(B * Hkv * used, page, 128)
+    tab = torch.full((B, Hkv, mp), -1, dtype=torch.int32, device="cuda")
+    tab[:, :, :used] = torch.randperm(B * Hkv * used, generator=g, device="cuda").view(B, Hkv, used).int()
+    ln = torch.full((B, Hkv), rows, dtype=torch.int32, device="cuda")
+    return dict(q=q, Kc=Kp, Vc=Vp, length=ln, Kd=Kd, Vd=Vd, table=tab, max_len=expected)
+
+
+@pytest.mark.parametrize("B,H,Hkv,T,rows,expected,launches", FORMS)
+def test_tree_form_and_workspace(B, H, Hkv, T, rows, expected, launches):
+    """The form goes by the sizes; none reads what the workspace held or writes behind what it asked for."""
+    a = _form(B, H, Hkv, T, rows, expected)
+    d = L.tree_dims(a["q"], a["Kc"], a["table"], a["Kd"], max_len=expected)
+    n = L.workspace_bytes(L.OP_TREE_ATTN, d)
+    outs = []
+    for fill in (0xFF, 0x00):                                        # NaN, zeros
+        ws = torch.full((n + 4096,), fill, dtype=torch.uint8, device="cuda")
+        if not outs:
+            assert count_launches(lambda: L.tree_attn(**a, ws=ws[:n])) == launches
+        outs.append(L.tree_attn(**a, ws=ws[:n], want_lse=True))
+        assert ws[n:].eq(fill).all()
+    assert same(outs[0][0], outs[1][0]) and torch.equal(outs[0][1], outs[1][1])
+    j = torch.arange(rows, device="cuda")
+    at = a["table"][:, :, j // 64].long() * 64 + j % 64
+    K = torch.cat([a["Kc"].view(-1, 128)[at], a["Kd"]], 2).double().repeat_interleave(H // Hkv, 1)
+    V = torch.cat([a["Vc"].view(-1, 128)[at], a["Vd"]], 2).double().repeat_interleave(H // Hkv, 1)
+    x = torch.einsum("bthd,bhnd->bhtn", a["q"].double(), K) / 128 ** 0.5
+    x[..., rows:].masked_fill_(~torch.ones(T, T, dtype=torch.bool, device="cuda").tril(), -torch.inf)
+    want = torch.einsum("bhtn,bhnd->bthd", torch.softmax(x, -1), V)
+    o_tol, l_tol = tree_bound(f64(a["q"]), f64(K), f64(V), rows + T, 1 / np.sqrt(128))
+    assert ((outs[0][0].double() - want).abs() <= 2.0 ** -8 * want.abs() + o_tol).all()
+    lse = torch.logsumexp(x, -1)
+    assert ((outs[0][1].double() - lse).abs() <= l_tol + 2.0 ** -22 * lse.abs()).all()
+
+
+@pytest.mark.parametrize("case", [FORMS[0], FORMS[1], FORMS[3], FORMS[5], FORMS[6]])
+def test_tree_waits_that_run_out(case):
+    """Copies of the keys that never come: the call ends, says so, and the next one is right again."""
+    a = _form(*case[:6])
+    try:
+        L.use_library(BU.build_test())
+        st = flag()
+        L.lib().lvlm_debug_starve_tree(1)
+        L.tree_attn(**a, dev_status=st)
+        torch.cuda.synchronize()
+        assert st.item() & L.DEV_TIMEOUT
+        L.lib().lvlm_debug_starve_tree(0)
+        st.zero_()
+        got, _ = L.tree_attn(**a, dev_status=st)
+        torch.cuda.synchronize()
+        assert st.item() == 0
+        L.lib().lvlm_debug_set_pdl(0)                                # and programmatic dependent launch changes nothing
+        off, _ = L.tree_attn(**a)
+        torch.cuda.synchronize()
+        assert same(got, off)
+    finally:
+        L.lib().lvlm_debug_starve_tree(0)
+        L.lib().lvlm_debug_set_pdl(1)
+        L.use_library(None)
+    again, _ = L.tree_attn(**a)
+    assert same(again, got)
+
+
+def test_lengths_grow_where_they_lie():
+    """One token a call into a paged cache, the length read and written by the same kernel, forty times over."""
+    r = np.random.default_rng(31)
+    B, Hkv, page, mp = 3, 4, 16, 5
+    K = torch.zeros(B * Hkv * mp, page, 128, dtype=BF, device="cuda")
+    V = torch.zeros_like(K)
+    tab = dev(r.permutation(B * Hkv * mp).reshape(B, Hkv, mp))
+    start = r.integers(0, 30, size=(B, Hkv))
+    ln, st = dev(start), flag()
+    new = bf(r, 40, B, 1, Hkv, 128).cuda()
+    count = dev([1, 0, 1])
+    for i in range(40):
+        L.rope_append(new[i], new[i], None, None, K, V, ln, table=tab, count=count, dev_status=st)
+    assert st.item() == 0 and np.array_equal(i32(ln), start + 40 * np.array([[1], [0], [1]]))
+    lg = logical(K, tab)
+    for b in (0, 2):
+        for g in range(Hkv):
+            assert same(lg[b, g, start[b, g]:start[b, g] + 40], new[:, b, 0, g])
+    assert count_launches(lambda: L.rope_append(new[0], new[0], None, None, K, V, ln, table=tab, count=count)) == 1
