@@ -369,11 +369,27 @@ def _arg(t: Optional[torch.Tensor], name: str, dtype, shape, device: int):
     return t.data_ptr()
 
 
-def _rows(t: torch.Tensor, name: str, shape, strides, device: int):
-    """Pointer of a bf16 argument of which only the rows of D channels have to be contiguous."""
-    if t.dtype is not _BF16 or t.get_device() != device or (shape is not None and t.shape != shape) or strides[-1] != 1:
-        _refuse(t, name, _BF16, shape, device, True)
-    return t.data_ptr()
+def _pair(K: torch.Tensor, V: torch.Tensor, names, D: int, device: int):
+    """Shape, strides and pointers of two bf16 tensors laid out alike, of which only the rows of D channels have to be contiguous."""
+    shape, st = K.shape, K.stride()
+    if (K.dtype is not _BF16 or V.dtype is not _BF16 or K.get_device() != device or V.get_device() != device or V.shape != shape
+            or V.stride() != st or st[-1] != 1 or shape[-1] != D):
+        for t, name in zip((K, V), names):
+            if t.dtype != _BF16 or t.get_device() != device or t.shape != shape or t.stride(-1) != 1:
+                _refuse(t, name, _BF16, shape, device, True)
+        if shape[-1] != D:
+            raise ValueError(f"{names[0]} has rows of {shape[-1]} channels, the other tensors of {D}")
+        raise ValueError(f"{names[0]} and {names[1]} have to have the same strides")
+    return shape, st, K.data_ptr(), V.data_ptr()
+
+
+def _queries(d: Dims, q: torch.Tensor, shape, device: int):
+    """Pointer of the queries [B,T,H,D], whose rows of D channels have to be contiguous; fills their strides."""
+    st = q.stride()
+    if q.dtype is not _BF16 or q.get_device() != device or q.shape != shape or st[3] != 1:
+        _refuse(q, "q", _BF16, shape, device, True)
+    d.q_stride_b, d.q_stride_n, d.q_stride_h = _outer(q, "q", st, 3)
+    return q.data_ptr()
 
 
 def _outer(t: torch.Tensor, name: str, strides, n: int):
@@ -387,14 +403,15 @@ def _outer(t: torch.Tensor, name: str, strides, n: int):
     return st
 
 
+def _packed(names, shape, st):
+    if st[-2] != shape[-1] and shape[-2] > 1:
+        raise ValueError(f"the rows of {names[0]} and {names[1]} have to be packed")
+
+
 def _cache(d: Dims, Kc, Vc, table, B, Hkv, D, device: int):
     """Fills the cache's fields of ``d``; returns the three pointers."""
-    st, shape = Kc.stride(), tuple(Kc.shape)
-    kp, vp = _rows(Kc, "Kc", None, st, device), _rows(Vc, "Vc", shape, st, device)
-    if Vc.stride() != st or st[-2] != shape[-1] and shape[-2] > 1:
-        raise ValueError("Kc and Vc have to have the same strides and packed rows")
-    if shape[-1] != D:
-        raise ValueError(f"Kc has rows of {shape[-1]} channels, the new tokens of {D}")
+    shape, st, kp, vp = _pair(Kc, Vc, ("Kc", "Vc"), D, device)
+    _packed(("Kc", "Vc"), shape, st)
     if table is None:
         if len(shape) != 4 or shape[0] != B or shape[1] != Hkv:
             raise ValueError(f"a contiguous cache has the shape [{B}, {Hkv}, cap, D], not {tuple(shape)}")
@@ -405,20 +422,19 @@ def _cache(d: Dims, Kc, Vc, table, B, Hkv, D, device: int):
     if len(shape) != 3 or len(t_shape) != 3:
         raise ValueError("a paged cache has the shape [n_pages, page, D], its table [B, Hkv, max_pages]")
     d.n_pages, d.page, _ = shape
-    d.page_stride = _outer(Kc, "Kc", st, 2)[0]
+    d.page_stride = st[0] if st[0] and not st[0] & 7 else _outer(Kc, "Kc", st, 2)[0]
     d.max_pages = n = t_shape[2]
     return kp, vp, _arg(table, "table", _I32, (B, Hkv, n), device)
 
 
-def _drafts(d: Dims, Kd, Vd, shape, device: int):
+def _drafts(d: Dims, Kd, Vd, B, Hkv, D, device: int):
     """The same for a draft cache [B,Hkv,draft_cap,D]."""
-    st = Kd.stride()
-    kp = _rows(Kd, "Kd", shape, st, device)
-    if Vd is None:
-        raise ValueError("Kd without Vd")
-    vp = _rows(Vd, "Vd", shape, st, device)
-    if Vd.stride() != st or st[2] != shape[3] and shape[2] > 1:
-        raise ValueError("Kd and Vd have to have the same strides and packed rows")
+    if Kd is None or Vd is None:
+        raise ValueError("Kd and Vd go together")
+    shape, st, kp, vp = _pair(Kd, Vd, ("Kd", "Vd"), D, device)
+    if len(shape) != 4 or shape[0] != B or shape[1] != Hkv:
+        raise ValueError(f"a draft cache has the shape [{B}, {Hkv}, rows, D], not {tuple(shape)}")
+    _packed(("Kd", "Vd"), shape, st)
     d.draft_cap = shape[2]
     d.draft_stride_b, d.draft_stride_h = _outer(Kd, "Kd", st, 2)
     return kp, vp
@@ -465,28 +481,24 @@ def rope_append(k_new, v_new, pos, cos_sin, Kc, Vc, length=None, *, q=None, q_ou
     pos is [B,T], or [3,B,T] with ``sections`` (the frequencies that follow each axis); cos_sin None: nothing is rotated.
     Returns q_out [B,T,H,D] (``q_out=q`` rotates in place) or None without q."""
     dev = _here(k_new)
-    shape, st = tuple(k_new.shape), k_new.stride()
-    B, T, Hkv, D = shape
+    B, T, Hkv, D = k_new.shape
+    _, st, knp, vnp = _pair(k_new, v_new, ("k_new", "v_new"), D, dev)
     d = Dims()
     d.B, d.Hkv, d.D, d.T, d.interleaved = B, Hkv, D, T, bool(interleaved)
     kp, vp, tp = _cache(d, Kc, Vc, table, B, Hkv, D, dev)
-    knp, vnp = _rows(k_new, "k_new", None, st, dev), _rows(v_new, "v_new", shape, st, dev)
-    if v_new.stride() != st:
-        raise ValueError("k_new and v_new have to have the same strides")
     d.new_stride_b, d.new_stride_n, d.new_stride_h = _outer(k_new, "k_new", st, 3)
     qp = qop = None
     if q is not None:
         d.H = H = q.shape[2]
-        q_st, q_shape = q.stride(), (B, T, H, D)
-        qp = _rows(q, "q", q_shape, q_st, dev)
-        d.q_stride_b, d.q_stride_n, d.q_stride_h = _outer(q, "q", q_st, 3)
+        q_shape = (B, T, H, D)
+        qp = _queries(d, q, q_shape, dev)
         if q_out is q:
             qop = qp
         else:
             if q_out is None:
-                q_out = torch.empty(B, T, H, D, dtype=_BF16, device=q.device)
+                q_out = torch.empty(q_shape, dtype=_BF16, device=q.device)
             qop = _arg(q_out, "q_out", _BF16, q_shape, dev)
-            if qop == qp and q_out.stride() != q_st:
+            if qop == qp and q_out.stride() != q.stride():
                 raise ValueError("q_out starts where q does but is laid out differently")
     elif q_out is not None:
         raise ValueError("q_out without q")
@@ -517,13 +529,12 @@ def commit_rows(Kd, Vd, Kc, Vc, length, count=None, *, index=None, table=None, l
     grows by ``count``: in place, or into ``len_out``.  count [B] (None = all) or, to move a ragged cache, [B,Hkv];
     index [B,T] int32, None = the first rows."""
     dev = _here(Kd)
-    shape = tuple(Kd.shape)
-    B, Hkv, rows, D = shape
+    B, Hkv, rows, D = Kd.shape
     T = rows if index is None else index.shape[-1]
     d = Dims()
     d.B, d.Hkv, d.D, d.T = B, Hkv, D, T
     kp, vp, tp = _cache(d, Kc, Vc, table, B, Hkv, D, dev)
-    kdp, vdp = _drafts(d, Kd, Vd, shape, dev)
+    kdp, vdp = _drafts(d, Kd, Vd, B, Hkv, D, dev)
     hs = (B, Hkv)
     d.count_heads = count is not None and count.dim() == 2
     lp = _arg(length, "length", _I32, hs, dev)
@@ -557,19 +568,16 @@ def tree_attn(q, Kc, Vc, length, *, Kd=None, Vd=None, mask=None, count=None, tab
     [B]: drafts of each sequence (None = T).  max_len: rows a head is expected to hold at most, where the caller knows (it decides
     how the work is split, not the result).  Returns (out [B,T,H,D], lse [B,H,T] or None); rows behind count are left as they were."""
     dev = _here(q)
-    shape, q_st = tuple(q.shape), q.stride()
+    shape = q.shape
     B, T, H, D = shape
     Hkv = Kc.shape[1] if table is None else table.shape[1]
     d = Dims()
     d.B, d.H, d.Hkv, d.D, d.T, d.N = B, H, Hkv, D, T, max_len or 0
-    qp = _rows(q, "q", None, q_st, dev)
-    d.q_stride_b, d.q_stride_n, d.q_stride_h = _outer(q, "q", q_st, 3)
+    qp = _queries(d, q, shape, dev)
     kp, vp, tp = _cache(d, Kc, Vc, table, B, Hkv, D, dev)
     kdp = vdp = None
-    if Kd is not None:
-        kdp, vdp = _drafts(d, Kd, Vd, (B, Hkv, Kd.shape[2], D), dev)
-    elif Vd is not None:
-        raise ValueError("Vd without Kd")
+    if Kd is not None or Vd is not None:
+        kdp, vdp = _drafts(d, Kd, Vd, B, Hkv, D, dev)
     mp = None
     if mask is not None:
         W = (T + 31) // 32
