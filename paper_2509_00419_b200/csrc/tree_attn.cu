@@ -426,8 +426,8 @@ static bool tree_layout(const lvlm_dims* d, int64_t cap, TreeLayout* L) {
     const int unit_tiles = tree_unit_tiles(heads, tiles, keys), tc_units = (tiles + unit_tiles - 1) / unit_tiles;
     const int64_t units = heads * tc_units;
     int64_t parts = units < kTreeTcCtas ? kTreeTcCtas / units : 1;
-    const int64_t most = tc_steps / 2;                       // (two key tiles or more a part: one, and more parts, is no faster)
-    parts = parts > most ? (most > 0 ? most : 1) : parts;
+    const int64_t most = (tc_steps + 1) / 2;                 // (two key tiles a part: one, and more parts, is no faster)
+    parts = parts > most ? most : parts;
     // More units than SMs: a CTA each, in waves, or runs.  Estimates of either in us, for equal lengths (us measured, waves / runs): 256 units of
     // two row tiles, 216 keys 40 / 52, 1100 72 / 85, 3008 153 / 164, 9000 440 / 479; 160 of one, 1100 keys 46 / 53, 9000 232 / 151; 224
     // of two, 3008 keys 150 / 143, 16640 700 / 577.
