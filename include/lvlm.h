@@ -349,6 +349,7 @@ lvlm_status lvlm_decode_attn_static(const void* q, void* Kc, void* Vc, int32_t* 
  *   K[b,g,len[b,g] + t]   = rot(k_new[b,t,g])       k_new, v_new [B][T][Hkv][D] (strides d->new_stride_*)
  *   V[b,g,len[b,g] + t]   = v_new[b,t,g]            for t < count[b]
  *   len_out[b,g]          = len[b,g] + count[b]
+ * k_new and v_new may not overlap the cache.  A row that is skipped for its page counts in len_out all the same.
  *   pos        [axes][B][T] int32, positions of the tokens; one outside [0, n_pos) sets LVLM_DEV_BOUNDS and leaves the
  *              channels that follow it as they are
  *   cos_sin    [n_pos][rot] fp32, 16-byte aligned; cos_sin and pos are only needed with rot > 0

@@ -447,6 +447,15 @@ def _here(t: torch.Tensor) -> int:
     return torch._C._cuda_getDevice()
 
 
+def _new(make, stream):
+    """What ``make`` allocates, on the stream that will use it: memory of the current stream may still be read there, and is handed
+    out again there as soon as it is freed."""
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        return make()
+
+
 def rope_table(n_pos: int, rot: int = 128, base: float = 10000.0, device="cuda") -> torch.Tensor:
     """cos_sin [n_pos, rot] fp32 for ``rope_append``: cosines of the rot/2 frequencies base^(-2i/rot), then their sines.
     The angles are formed in 64 bits: in 32 an angle of position p is off by p 2^-24 radians."""
@@ -496,7 +505,7 @@ def rope_append(k_new, v_new, pos, cos_sin, Kc, Vc, length=None, *, q=None, q_ou
             qop = qp
         else:
             if q_out is None:
-                q_out = torch.empty(q_shape, dtype=_BF16, device=q.device)
+                q_out = _new(lambda: torch.empty(q_shape, dtype=_BF16, device=q.device), stream)
             qop = _arg(q_out, "q_out", _BF16, q_shape, dev)
             if qop == qp and q_out.stride() != q.stride():
                 raise ValueError("q_out starts where q does but is laid out differently")
@@ -586,11 +595,11 @@ def tree_attn(q, Kc, Vc, length, *, Kd=None, Vd=None, mask=None, count=None, tab
     if scale is None:
         scale = 1.0 / math.sqrt(D)
     if out is None:
-        out = torch.empty(B, T, H, D, dtype=_BF16, device=q.device)
+        out = _new(lambda: torch.empty(B, T, H, D, dtype=_BF16, device=q.device), stream)
     if lse is None and want_lse:
-        lse = torch.empty(B, H, T, dtype=_F32, device=q.device)
+        lse = _new(lambda: torch.empty(B, H, T, dtype=_F32, device=q.device), stream)
     if ws is None:
-        ws = alloc_workspace(OP_TREE_ATTN, d, q.device)
+        ws = _new(lambda: alloc_workspace(OP_TREE_ATTN, d, q.device), stream)
     elif ws.get_device() != dev:
         raise ValueError(f"ws is on {ws.device}, the current device is cuda:{dev}")
     _check(lib().lvlm_tree_attn(qp, kp, vp, tp, _arg(length, "length", _I32, (B, Hkv), dev), kdp, vdp, mp,

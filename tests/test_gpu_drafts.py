@@ -624,6 +624,30 @@ def test_two_calls_at_once():
         assert same(out, alone)
 
 
+def test_what_a_call_allocates_belongs_to_its_stream():
+    """Results and workspace that the calls make themselves, on a stream that is behind: memory that the current stream asks for
+    meanwhile is other memory."""
+    r = np.random.default_rng(6)
+    B, H, Hkv, T, cap = 2, 8, 2, 40, 3000
+    q, Kc, Vc, Kd, Vd = [x.cuda() for x in (bf(r, B, T, H, 128), bf(r, B, Hkv, cap, 128), bf(r, B, Hkv, cap, 128), bf(r, B, Hkv, T, 128), bf(r, B, Hkv, T, 128))]
+    k, v = (bf(r, B, T, Hkv, 128).cuda() for _ in range(2))
+    ln, pos, cs = dev(r.integers(cap // 2, cap, size=(B, Hkv))), dev(r.integers(0, 500, size=(B, T))), L.rope_table(512)
+    want, want_lse = L.tree_attn(q, Kc, Vc, ln, Kd=Kd, Vd=Vd, want_lse=True)
+    Ka, Va = torch.zeros_like(Kd), torch.zeros_like(Vd)
+    want_q = L.rope_append(k, v, pos, cs, Ka, Va, q=q)
+    size = L.alloc_workspace(L.OP_TREE_ATTN, L.tree_dims(q, Kc, None, Kd), "cuda").numel()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    with torch.cuda.stream(s):
+        torch.cuda._sleep(20_000_000)
+    got, lse = L.tree_attn(q, Kc, Vc, ln, Kd=Kd, Vd=Vd, want_lse=True, stream=s)
+    got_q = L.rope_append(k, v, pos, cs, Ka, Va, q=q, stream=s)
+    held = [torch.full((size,), 0x7F, dtype=torch.uint8, device="cuda") for _ in range(3)]      # as large as the workspace that was let go
+    torch.cuda.current_stream().synchronize()
+    s.synchronize()
+    assert len(held) == 3 and same(got, want) and same(got_q, want_q) and torch.equal(lse, want_lse)
+
+
 # ---- forms, workspaces, waits ----------------------------------------------------------------------------------------
 FORMS = [  # B, H, Hkv, T, rows, expected rows, launches
     (1, 28, 4, 1, 300, None, 1), (2, 32, 8, 8, 400, None, 1),          # mma.sync, clusters
