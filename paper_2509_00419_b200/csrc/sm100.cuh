@@ -48,24 +48,21 @@ __device__ __forceinline__ bool mbar_try(uint64_t* bar, uint32_t parity) {
         : "=r"(done) : "r"(smem_u32(bar)), "r"(parity) : "memory");
     return done != 0;
 }
-// One poll that, where it finds the phase incomplete, parks the thread for a moment.
-__device__ __forceinline__ bool mbar_try_for(uint32_t addr, uint32_t parity) {
-    uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(done) : "r"(addr), "r"(parity), "r"(64u) : "memory");
-    return done != 0;
-}
 // Returns false if the phase with the given parity did not complete within the poll limit.  A poll that finds
 // the phase incomplete parks the thread for a moment (it resumes as soon as the phase completes),
 // so that waiting warps leave the issue slots to the warps that work.
 __device__ __forceinline__ bool mbar_wait(uint64_t* bar, uint32_t parity) {
     const uint32_t addr = smem_u32(bar);
 #pragma unroll 1
-    for (uint32_t it = 0; it < kSpinLimit; ++it)
-        if (mbar_try_for(addr, parity)) return true;
+    for (uint32_t it = 0; it < kSpinLimit; ++it) {
+        uint32_t done;
+        asm volatile(
+            "{\n\t.reg .pred p;\n\t"
+            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n\t"
+            "selp.u32 %0, 1, 0, p;\n\t}"
+            : "=r"(done) : "r"(addr), "r"(parity), "r"(64u) : "memory");
+        if (done) return true;
+    }
     return false;
 }
 

@@ -1,8 +1,8 @@
 // lvlm_tree_attn, many query rows or long caches: tcgen05.
 //
 // The T G query rows of a KV head lie in tiles of up to 128 rows, floor(128 / G) drafts with all heads of the group.  A unit of work is
-// two row tiles of a head that take turns at the tensor cores against its key tiles (128 keys: the cache, then the drafts), or the odd
-// row tile out, whose key tiles the two halves of a CTA take in turn and whose results they add at the end:
+// two row tiles of a head that take turns at the tensor cores against its key tiles (128 keys: the cache, then the drafts), or one row
+// tile, whose key tiles the two halves of a CTA take in turn and whose results they add at the end:
 //   S = Q K_j^T      operands by TMA (128-byte swizzle; a box per page where the cache is paged), 128x128 fp32 in tensor memory
 //   softmax          thread = query row, running maximum and sum in the log2 domain; probabilities go back as bf16 head + bf16
 //                    remainder over the logits they came from (a plain bf16 would cost as much again as the rounding of the result)
@@ -13,6 +13,9 @@
 // a unit each, and the other warps work through them without stopping in between (the keys of the next segment are fetched during
 // the epilogue of this one).
 // A unit that is cut leaves its parts (max, sum, output) in the workspace; tree_combine_kernel adds them in order.
+// What bounds it: long calls the MMAs, 48 of 128x128x16 a turn of both row tiles, a third of them for the remainders of P.  16 sequences of up to
+// 244 rows x 1888 keys 53 us (tensor pipe active 0.69 of the time on the busiest SM, which includes start and end), 4 of 1536 rows x 16640
+// keys 580 us (1080 TFLOP/s, remainders counted).  Short calls: latency; of 16 us (104 rows x 3008 keys) the combining launch is 2.4.
 // Rows of V behind the end of the cache or of the drafts are zeroed in shared memory before they are multiplied: they may hold
 // anything, and their weight of zero would not stop a NaN.
 #include "exp2.cuh"
@@ -51,7 +54,7 @@ struct TreeTcSmem {
     float xm[2][kTT], xl[2][kTT];            // one row tile: (max, sum) of a row over the key tiles of either half
 };
 
-// One short loop: the kernel runs through most of its code once, so that code fetched is time spent.
+// Bounded: a wait that runs out sets the status, and the waits after it give up at once.
 __device__ __forceinline__ bool tree_wait(uint64_t* bar, uint32_t parity, TreeTcSmem* sm, const TreeArgs& a) {
     if (mbar_try(bar, parity)) return true;
     if (sm->abort) return false;
