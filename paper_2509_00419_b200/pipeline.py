@@ -188,7 +188,7 @@ class PagedLayers:
     """KV caches of several layers in one pool of pages, ragged per (layer, sequence, KV head): what a compression evicts is free
     memory.  ``pack`` takes over the contiguous caches of a ``DecodeLayers``; a step then runs, per layer, a tree of up to T
     drafted tokens (``draft_layer``: rotation, draft cache, attention over cache and drafts), and ``commit`` appends the accepted ones
-    of all layers.  A head's pages are handed out by ``reserve`` on the host, ahead of the rows that need them."""
+    of all layers.  A head's pages are handed out by ``reserve`` on the host, ahead of the rows that need them, and come back with ``release``."""
 
     def __init__(self, n_layers, B, H, Hkv, n_pages, page, max_pages, T, device, rot=128):
         self.nl, self.B, self.H, self.Hkv, self.page, self.T, self.rot, self.device = n_layers, B, H, Hkv, page, T, rot, device
@@ -221,6 +221,17 @@ class PagedLayers:
                 self._table[l, b, g, j] = self._free.pop()
         self._held = torch.maximum(self._held, need)
         self.table.copy_(self._table)
+
+    def release(self, b: int):
+        """Sequence ``b`` is finished: its pages are free again and its lengths 0.  Calls before this one in the stream still see them."""
+        if not 0 <= b < self.B:
+            raise IndexError(f"there are {self.B} sequences, none is number {b}")
+        held = self._table[:, b]
+        self._free += held[held >= 0].tolist()[::-1]
+        held.fill_(-1)
+        self._held[:, b] = 0
+        self.table[:, b].copy_(held)
+        self.len[:, b].zero_()
 
     def pages_free(self) -> int:
         return len(self._free)

@@ -204,3 +204,35 @@ def test_tree_workspace_never_shrinks(lib, heads):
         sizes = [size(*x) for x in line]
         for i in range(1, len(line)):
             assert sizes[i] >= sizes[i - 1], (line[i - 1], line[i])
+
+
+def test_pages_come_back():
+    """Pages are handed out once, a finished sequence gives all of its own back, and the others keep theirs."""
+    from paper_2509_00419_b200.pipeline import PagedLayers
+
+    c = PagedLayers(2, 3, 4, 2, n_pages=40, page=16, max_pages=5, T=4, device="cpu")
+    rows = torch.tensor([[[17, 1], [0, 80], [33, 16]]] * 2)
+    c.reserve(rows)
+    need = (rows + 15) // 16
+    used = c.table[c.table >= 0].tolist()
+    assert len(used) == len(set(used)) == int(need.sum()) and c.pages_free() == 40 - len(used)
+    assert torch.equal((c.table >= 0).sum(3), need)
+    c.len.copy_(rows)
+    before = c.table.clone()
+    c.release(1)
+    assert (c.table[:, 1] == -1).all() and (c.len[:, 1] == 0).all() and c.pages_free() == 40 - int(need[:, [0, 2]].sum())
+    for b in (0, 2):
+        assert torch.equal(c.table[:, b], before[:, b]) and torch.equal(c.len[:, b].long(), rows[:, b])
+    c.release(1)                                       # nothing is given back twice
+    assert c.pages_free() == 40 - int(need[:, [0, 2]].sum())
+    c.reserve(rows)
+    used = c.table[c.table >= 0].tolist()
+    assert len(used) == len(set(used)) == int(need.sum())
+    with pytest.raises(IndexError):
+        c.release(3)
+    free, table = c.pages_free(), c.table.clone()
+    with pytest.raises(RuntimeError):
+        c.reserve(torch.full((2, 3, 2), 80))           # more than there are: nothing is handed out
+    with pytest.raises(ValueError):
+        c.reserve(torch.full((2, 3, 2), 81))
+    assert c.pages_free() == free and torch.equal(c.table, table)
