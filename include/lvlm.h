@@ -400,8 +400,9 @@ lvlm_status lvlm_commit_rows(const void* Kd, const void* Vd, const int32_t* inde
  * Rows behind len and behind count may hold anything, NaN included; the rows in front of them are finite.
  * d->N, optional: how many rows the caller expects a head to hold at most (0 = unknown): how the work is split over the GPU then
  * goes by it instead of the capacity.  It changes no result beyond rounding.
- * Workspace: the partial results where a head's keys are split; lvlm_workspace_bytes(LVLM_OP_TREE_ATTN, d).  Calls that may
- * overlap on the GPU need workspaces of their own.
+ * Workspace: the partial results where a head's keys are split, 28.3 MB (2^20) and 8 bytes a head and 128 rows at most.
+ * lvlm_workspace_bytes(LVLM_OP_TREE_ATTN, d) is enough for d and for every smaller problem; a call is refused less only where it would use
+ * it, and one that splits nothing takes ws = NULL.  Calls that may overlap on the GPU need workspaces of their own.
  * Reads d: B,H,Hkv,D,N,T,draft_cap,mask_shared,q_stride_*,draft_stride_*, and the cache's fields.
  * Errors: INVALID_ARG (NULL q/Kc/Vc/len/out, one of Kd/Vd, a mask without drafts, draft_cap < T, scale <= 0), UNSUPPORTED
  * (D != 128, T > 256, H/Hkv > 64), ALIGNMENT, WORKSPACE.  Contents of out and lse are undefined when a kernel gave up on a

@@ -312,7 +312,7 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
 // 4 units of 37 parts: 9.5 us with a warp going through all parts, 4.8 with four.
 constexpr int kTreeCombineWarps = 8;
 constexpr int kTreeMostParts = kTreeTcCtas;
-template <int CH, int SL>
+template <int CH, int SL, bool RUNS>
 __global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(const TreeArgs a) {
     __shared__ float s_m[kTreeMostParts][32], s_l[kTreeMostParts][32];
     __shared__ float4 s_v[SL > 1 ? kTreeCombineWarps : 1][32];
@@ -324,28 +324,34 @@ __global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(co
     pdl_enter();
     if (unit * a.unit_tiles * a.tile_rows >= h.n * a.G) return; // nothing asked for
     int2 of;                                                    // first slot and how many more parts
-    int stride;                                                 // slots between the CTAs of a unit's parts
-    if (a.runs) {
+    if (RUNS) {
         of = a.part_of[blockIdx.x];
-        stride = 2;
     } else {
         const int step = tree_part(h, a.S);
         of = make_int2(step >= h.nt ? -1 : hd * a.S * a.units + unit, (h.nt - 1) / step);
-        stride = a.units;
     }
     if (of.x < 0) return;                                       // not cut
     const int r = tile * a.tile_rows + row, t = r / a.G;
     const bool mine = row < a.tile_rows && t < h.n;
     const int c0 = (blockIdx.z * (kTreeCombineWarps / SL) + warp / SL) * CH, parts = min(of.y + 1, kTreeMostParts);
-    // (runs: part p >= 1 lies in the first slot of its CTA)
-    const int rest = a.runs ? of.x & ~1 : of.x;
-    auto slot = [&](int p) -> int64_t { return p == 0 ? of.x : rest + stride * p; };
+    auto slot = [&](int p) -> int64_t { return RUNS ? (p == 0 ? kTreeTcCtas + of.x : of.x + p) : of.x + a.units * p; };
+    const int head = g * a.G + r % a.G;
+    uint2* to = reinterpret_cast<uint2*>(a.out + (((int64_t)b * a.T + t) * a.H + head) * kHeadDim) + c0;
     constexpr int kAhead = 16 / CH;
+    static_assert(!RUNS || SL == 1, "the thread that reads what lies in a row of out writes it");
     float4 x[kAhead][CH];
     auto fetch = [&](int p0) {                                  // parts p0, p0 + SL, ...
 #pragma unroll
         for (int u = 0; u < kAhead; ++u)
-            if (p0 + u * SL < parts) {
+            if (RUNS && p0 + u == 0) {                          // in two halves: see TreeArgs
+                const uint2* low = a.part_lo + (int64_t)of.x * (kHeadDim / 4) * a.pitch + place;
+#pragma unroll
+                for (int c = 0; c < CH; ++c) {
+                    const uint2 up = mine ? to[c] : make_uint2(0u, 0u), lo = low[(c0 + c) * a.pitch];
+                    x[u][c] = make_float4(__uint_as_float(__byte_perm(lo.x, up.x, 0x5410)), __uint_as_float(__byte_perm(lo.x, up.x, 0x7632)),
+                                          __uint_as_float(__byte_perm(lo.y, up.y, 0x5410)), __uint_as_float(__byte_perm(lo.y, up.y, 0x7632)));
+                }
+            } else if (p0 + u * SL < parts) {
                 const float4* from = reinterpret_cast<const float4*>(a.part_o + slot(p0 + u * SL) * a.pitch * kHeadDim) + place;
 #pragma unroll
                 for (int c = 0; c < CH; ++c) x[u][c] = from[(c0 + c) * a.pitch];
@@ -392,9 +398,7 @@ __global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(co
         }
     }
     if (!mine) return;
-    const int head = g * a.G + r % a.G;
     const float inv = Ls > 0.f ? 1.0f / Ls : 0.f;
-    uint2* to = reinterpret_cast<uint2*>(a.out + (((int64_t)b * a.T + t) * a.H + head) * kHeadDim) + c0;
 #pragma unroll
     for (int c = 0; c < CH; ++c) to[c] = make_uint2(pack_bf16(v[c].x * inv, v[c].y * inv), pack_bf16(v[c].z * inv, v[c].w * inv));
     if (a.lse && c0 == 0) a.lse[((int64_t)b * a.H + head) * a.T + t] = Ls > 0.f ? (M + log2f(Ls)) * kTreeLn2 : -INFINITY;
@@ -407,12 +411,33 @@ static int tree_unit_tiles(int64_t heads, int tiles, int64_t keys) {
     return tiles > 1 && (heads * tiles > kTreeTcCtas || (keys > 16000 && heads * tiles >= 32)) ? 2 : 1;
 }
 
-// How a call is carried out.  `total` is what a caller is told, whichever form it is, so that it never shrinks as a problem grows.
+// How a call is carried out.  `need` is what this form uses, `total` what a caller is told: at least what any problem that is no larger
+// uses, so that it never shrinks as a problem grows.
 struct TreeLayout {
     int tc, R, runs, S, unit_tiles, units, pitch;
     int64_t ctas;
-    size_t off_o, off_of, total;
+    size_t off_o, off_lo, off_of, need, total;
 };
+
+// Bytes of the parts of units, and of runs: rows of (max, sum), of outputs, of the lower halves of those that begin a unit, and who has them.
+static size_t parts_bytes(int64_t places) { return align_up((size_t)places * 8, 256) + (size_t)places * kHeadDim * 4; }
+static size_t runs_bytes(int64_t pitch, int64_t units) {
+    return (size_t)kTreeTcCtas * pitch * (2 * 8 + kHeadDim * 4 + kHeadDim * 2) + align_up((size_t)units * 8, 256);
+}
+static void tree_workspace(TreeLayout* L, int64_t heads) {
+    const size_t places = (size_t)kTreeTcCtas * L->pitch;                    // a slot a CTA (a multiple of 256 bytes of anything)
+    if (L->runs) {
+        L->off_o = 2 * places * 8;
+        L->off_lo = L->off_o + places * kHeadDim * 4;
+        L->off_of = L->off_lo + places * kHeadDim * 2;
+        L->need = runs_bytes(L->pitch, heads * L->units);
+    } else {
+        const int64_t used = L->tc && L->S > 1 ? heads * L->units * L->S * L->pitch : 0;
+        L->off_o = align_up((size_t)used * 8, 256);
+        L->off_lo = L->off_of = 0;
+        L->need = used ? parts_bytes(used) : 0;
+    }
+}
 
 static bool tree_layout(const lvlm_dims* d, int64_t cap, TreeLayout* L) {
     if (d->B <= 0 || d->H <= 0 || d->Hkv <= 0 || d->H % d->Hkv || d->T <= 0 || d->T > kTreeMaxT || d->H / d->Hkv > kTreeMaxGroup || cap <= 0) return false;
@@ -453,10 +478,13 @@ static bool tree_layout(const lvlm_dims* d, int64_t cap, TreeLayout* L) {
     L->units = tc_units;
     L->pitch = unit_tiles * kTreeTcRows;
     L->ctas = !L->tc ? heads * S : L->runs ? kTreeTcCtas : units * parts;
-    const int64_t places = (int64_t)2 * kTreeTcCtas * (tiles > 1 ? 2 : 1) * kTreeTcRows;       // two slots a CTA
-    L->off_o = align_up((size_t)places * 8, 256);
-    L->off_of = L->off_o + (size_t)places * kHeadDim * 4;
-    L->total = align_up(L->off_of + (size_t)(heads * tiles) * 8, 256);
+    if (!L->tc) L->runs = 0;
+    tree_workspace(L, heads);
+    // The largest problem's: parts are no more than the CTAs, nor than half the key tiles of a cache of any length up to its capacity.
+    const int64_t cap_steps = (cap + kTreeTcRows - 1) / kTreeTcRows + (drafts + kTreeTcRows - 1) / kTreeTcRows;
+    const int64_t pitch = (tiles > 1 ? 2 : 1) * kTreeTcRows, slots = heads * tiles * ((cap_steps + 1) / 2);
+    const size_t parted = parts_bytes((slots < kTreeTcCtas ? slots : kTreeTcCtas) * pitch), in_runs = runs_bytes(pitch, heads * tiles);
+    L->total = heads * tiles > kTreeTcCtas && in_runs > parted ? in_runs : parted;
     return true;
 }
 
@@ -505,7 +533,15 @@ extern "C" lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void*
         return LVLM_ERR_ALIGNMENT;
     TreeLayout L;
     if (!tree_layout(d, a.c.cap, &L)) return LVLM_ERR_INVALID_ARG;
-    if (!ws || !aligned256(ws) || ws_bytes < L.total) return LVLM_ERR_WORKSPACE;
+    // In runs a part lies in `out` while other CTAs may still fetch the queries of its unit: where out is q, units go in waves.
+    if (L.runs && out == q) {
+        if ((int64_t)d->B * d->Hkv > 65535) return LVLM_ERR_INVALID_ARG;
+        L.runs = 0;
+        L.S = 1;
+        L.ctas = (int64_t)d->B * d->Hkv * L.units;
+        tree_workspace(&L, (int64_t)d->B * d->Hkv);
+    }
+    if (L.need && (!ws || !aligned256(ws) || ws_bytes < L.need)) return LVLM_ERR_WORKSPACE;
     char* wsb = static_cast<char*>(ws);
     TreeMaps m;
     {
@@ -531,6 +567,7 @@ extern "C" lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void*
     a.scale_log2 = scale * kTreeLog2e;
     a.part_ml = reinterpret_cast<float2*>(wsb);
     a.part_o = reinterpret_cast<float*>(wsb + L.off_o);
+    a.part_lo = reinterpret_cast<uint2*>(wsb + L.off_lo);
     a.part_of = reinterpret_cast<int2*>(wsb + L.off_of);
     a.dev_status = dev_status;
 #ifdef LVLM_TEST_HOOKS
@@ -553,7 +590,8 @@ extern "C" lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void*
     const int64_t units = (int64_t)d->B * d->Hkv * L.units;
     const unsigned blocks = (unsigned)(L.pitch / 32);
     const dim3 threads(kTreeCombineWarps * 32);
-    if (units * blocks * 16 <= 2 * kTreeTcCtas) return launch_kernel(tree_combine_kernel<1, 4>, dim3((unsigned)units, blocks, 16), threads, 0, stream, 1, a);
-    if (units * blocks * 4 <= kTreeTcCtas) return launch_kernel(tree_combine_kernel<1, 1>, dim3((unsigned)units, blocks, 4), threads, 0, stream, 1, a);
-    return launch_kernel(tree_combine_kernel<4, 1>, dim3((unsigned)units, blocks, 1), threads, 0, stream, 1, a);
+    if (L.runs) return launch_kernel(tree_combine_kernel<4, 1, true>, dim3((unsigned)units, blocks, 1), threads, 0, stream, 1, a);
+    if (units * blocks * 16 <= 2 * kTreeTcCtas) return launch_kernel(tree_combine_kernel<1, 4, false>, dim3((unsigned)units, blocks, 16), threads, 0, stream, 1, a);
+    if (units * blocks * 4 <= kTreeTcCtas) return launch_kernel(tree_combine_kernel<1, 1, false>, dim3((unsigned)units, blocks, 4), threads, 0, stream, 1, a);
+    return launch_kernel(tree_combine_kernel<4, 1, false>, dim3((unsigned)units, blocks, 1), threads, 0, stream, 1, a);
 }

@@ -24,11 +24,13 @@ struct TreeArgs {
     int pitch;               // places for the rows of a unit in a slot of the workspace
     int64_t q_sb, q_sn, q_sh;
     float scale_log2;
-    // Partial results.  A slot holds `pitch` rows, groups of four channels of all rows side by side.  Slot (head, part, unit), or with runs
-    // two slots a CTA, for its first segment and its last, and part_of [head, unit]: the first slot of a unit, -1 = it was not
-    // cut, and how many more CTAs have a part of it, in their first slots.
+    // Partial results.  A slot holds `pitch` rows, groups of four channels of all rows side by side.  Slot (head, part, unit).  With runs a
+    // CTA has at most one part that goes on with a unit, in slot `CTA`, and one that begins a unit, in slot kTreeTcCtas + CTA: of its fp32
+    // outputs the upper 16 bits lie in the rows of `out` that the unit ends in, only the lower ones in part_lo, so that the workspace
+    // stays below 32 MB.  part_of [head, unit]: the CTA that begins it, -1 = it was not cut, and how many more have a part of it.
     float2* part_ml;         // (max in the log2 domain, sum)
     float* part_o;           // output relative to that max
+    uint2* part_lo;          // lower 16 bits of four channels
     int2* part_of;
     CacheGeom c;
     int32_t* dev_status;

@@ -64,6 +64,9 @@ __device__ __forceinline__ bool tree_wait(uint64_t* bar, uint32_t parity, TreeTc
     return false;
 }
 
+// Halves of two words in one: their lower ones (selector 0x5410) or their upper ones (0x7632).
+__device__ __forceinline__ uint32_t halves(float x, float y, uint32_t selector) { return __byte_perm(__float_as_uint(x), __float_as_uint(y), selector); }
+
 // Row tiles of a head that are asked for, and what it weighs: a pair of them 2 a key tile, an odd one 1 (far below 2^31: a tile is
 // 64 KB); a head without keys one tile, so that its rows are written.
 __device__ __forceinline__ int tree_rt(const TreeHead& h, int tt) { return h.n <= tt ? (h.n > 0) : (h.n + tt - 1) / tt; }
@@ -342,7 +345,7 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
         long long at = lo, p = lo < hi ? sm->first_prefix : 0;    // how far I am; where head hd begins
         int hd = lo < hi ? sm->first_head : 0, s = 0;
         TreeHead h = sm->first;
-        bool ok = true, first = true;
+        bool ok = true;
         while (ok) {
             TreeSeg w;
             w.hd = -1;
@@ -362,12 +365,11 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
                 at = u0 + wt * nt;
                 if (t0 >= t1) continue;
                 w.hd = hd; w.tile = 2 * pair; w.t0 = t0; w.nk = h.nt > 0 ? t1 - t0 : 0; w.split = wt == 1; w.n = h.n; w.ln = h.ln;
-                w.slot = t0 == 0 && t1 == nt ? -1 : 2 * me + (first ? 0 : 1);
-                first = false;
+                w.slot = t0 > 0 ? me : t1 < nt ? kTreeTcCtas + me : -1;
                 if (t0 == 0 && lane == 0) {
-                    // where the parts of this unit lie: mine, then the first slots of the CTAs up to the one with its last tile
+                    // who has the parts of this unit: I, and the CTAs up to the one with its last tile
                     const long long z = u0 + wt * (nt - 1);
-                    a.part_of[(int64_t)hd * pairs + pair] = make_int2(w.slot, w.slot < 0 ? 0 : (int)((uint32_t)(z - lo) / (uint32_t)per));
+                    a.part_of[(int64_t)hd * pairs + pair] = w.slot < 0 ? make_int2(-1, 0) : make_int2(me, (int)((uint32_t)(z - lo) / (uint32_t)per));
                 }
             }
             ok = s < kTSegs || __all_sync(0xFFFFFFFFu, tree_wait(&sm->seg_empty[s % kTSegs], ((s / kTSegs) - 1) & 1, sm, a));
@@ -517,11 +519,12 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
             const uint32_t oa = split ? o_addr - u * kTT : o_addr;       // O of half 0, or of my tile
             const int c_lo = split ? 64 * u : 0, c_hi = split ? c_lo + 64 : kTT;     // one row tile: a half finishes half of the channels
             const int place = split ? row : u * kTT + row;
+            const bool begins = RUNS && w.slot >= kTreeTcCtas;           // (then w.slot is the place of its (max, sum) alone)
             const float inv = w.slot >= 0 ? 1.f : l_row > 0.f ? 1.0f / l_row : 0.f;
             f0 *= inv; f1 *= inv;
             const int my_at = mine ? t * a.H + row % G : -1;             // my row of the sequence's output
             __nv_bfloat16* out = a.out + ((int64_t)b * T * a.H + g * G) * kHeadDim + (lane & 3) * 8;
-            float4* part = reinterpret_cast<float4*>(a.part_o + (int64_t)w.slot * a.pitch * kHeadDim) + place;
+            float4* part = reinterpret_cast<float4*>(a.part_o) + (int64_t)w.slot * (kHeadDim / 4) * a.pitch + place;
             unsigned char* stage = sQ + (warp - 4) * 2048;
 #pragma unroll 1
             for (int c0 = c_lo; c0 < c_hi; c0 += 32) {                   // 32 channels at a time
@@ -537,17 +540,25 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
 #pragma unroll
                     for (int e = 0; e < 32; ++e) o[e] = f1 > 0.f ? fmaf(p[e], f1, o[e]) : o[e];
                 }
-                if (w.slot >= 0) {
+                if (w.slot >= 0 && !begins) {
                     // a part: groups of four channels of all rows side by side, so that the threads' stores are
 #pragma unroll
                     for (int q = 0; q < 8; ++q) part[(c0 / 4 + q) * a.pitch] = make_float4(o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]);
                 } else {
-                    // the rows themselves, through shared memory (the Q tile, which nobody needs any more)
+                    // the rows themselves, through shared memory (the Q tile, which nobody needs any more); of a part that begins a unit
+                    // the upper halves of its words
+                    if (begins) {
+                        uint2* low = a.part_lo + (int64_t)me * (kHeadDim / 4) * a.pitch + place;
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        *reinterpret_cast<uint4*>(stage + lane * 64 + ((q ^ (lane >> 1 & 3)) << 4)) =
-                            make_uint4(pack_bf16(o[8 * q], o[8 * q + 1]), pack_bf16(o[8 * q + 2], o[8 * q + 3]),
-                                       pack_bf16(o[8 * q + 4], o[8 * q + 5]), pack_bf16(o[8 * q + 6], o[8 * q + 7]));
+                        for (int q = 0; q < 8; ++q) low[(c0 / 4 + q) * a.pitch] = make_uint2(halves(o[4 * q], o[4 * q + 1], 0x5410), halves(o[4 * q + 2], o[4 * q + 3], 0x5410));
+                    }
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        uint32_t x[4];
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[i] = begins ? halves(o[8 * q + 2 * i], o[8 * q + 2 * i + 1], 0x7632) : pack_bf16(o[8 * q + 2 * i], o[8 * q + 2 * i + 1]);
+                        *reinterpret_cast<uint4*>(stage + lane * 64 + ((q ^ (lane >> 1 & 3)) << 4)) = make_uint4(x[0], x[1], x[2], x[3]);
+                    }
                     __syncwarp();
 #pragma unroll
                     for (int r0 = 0; r0 < 32; r0 += 8) {

@@ -206,6 +206,16 @@ def test_tree_workspace_never_shrinks(lib, heads):
             assert sizes[i] >= sizes[i - 1], (line[i - 1], line[i])
 
 
+def test_tree_workspace_is_small(lib):
+    """The widest trees over the longest caches fit 32 MiB, a token over a short cache asks for little."""
+    for H, Hkv in ((8, 8), (28, 4), (32, 8), (48, 8), (64, 1)):
+        for B_ in (1, 4, 32, 96):
+            for T in (1, 26, 61, 256):
+                for n in (216, 1888, 16640, 33000, 1 << 20):
+                    assert L.workspace_bytes(L.OP_TREE_ATTN, L.Dims(B=B_, H=H, Hkv=Hkv, D=128, T=T, draft_cap=T, cap=n)) <= 32 << 20
+    assert L.workspace_bytes(L.OP_TREE_ATTN, L.Dims(B=1, H=28, Hkv=4, D=128, T=1, draft_cap=1, cap=216)) <= 1 << 20
+
+
 def test_pages_come_back():
     """Pages are handed out once, a finished sequence gives all of its own back, and the others keep theirs."""
     from paper_2509_00419_b200.pipeline import PagedLayers

@@ -696,6 +696,43 @@ def test_tree_form_and_workspace(B, H, Hkv, T, rows, expected, launches):
     assert ((outs[0][1].double() - lse).abs() <= l_tol + 2.0 ** -22 * lse.abs()).all()
 
 
+def _least(a):
+    """The least workspace that a call is not refused, in steps of 256 bytes."""
+    lo, hi = 0, 32 << 12                                              # 32 MiB is enough for every form
+    ws = torch.empty(hi * 256, dtype=torch.uint8, device="cuda")
+    while lo < hi:
+        mid = (lo + hi) // 2
+        try:
+            L.tree_attn(**a, ws=ws[:mid * 256])
+            hi = mid
+        except L.LvlmError as e:
+            assert e.code == L.ERR_WORKSPACE
+            lo = mid + 1
+    return lo * 256
+
+
+@pytest.mark.parametrize("B,H,Hkv,T,rows,expected,launches", FORMS + [(10, 48, 8, 44, 200, 9000, 2), (1, 48, 8, 100, 3000, 20000, 2)])
+def test_tree_takes_what_its_form_needs(B, H, Hkv, T, rows, expected, launches):
+    """One launch: no workspace at all.  Two: what is said to be enough covers it, and with the least of it the result is the same,
+    whatever it held, and nothing behind it is written.  And with out = q."""
+    a = _form(B, H, Hkv, T, rows, expected)
+    want, want_lse = L.tree_attn(**a, want_lse=True)
+    least = _least(a)
+    assert (least > 0) == (launches == 2) and count_launches(lambda: L.tree_attn(**a)) == launches
+    assert least <= L.workspace_bytes(L.OP_TREE_ATTN, L.tree_dims(a["q"], a["Kc"], a["table"], a["Kd"], max_len=expected))
+    for fill in (0xFF, 0x00):
+        ws = torch.full((least + 4096,), fill, dtype=torch.uint8, device="cuda")
+        got, lse = L.tree_attn(**a, ws=ws[:least], want_lse=True)
+        assert same(got, want) and torch.equal(lse, want_lse) and ws[least:].eq(fill).all()
+    q = a["q"].clone()
+    got, lse = L.tree_attn(**{**a, "q": q}, out=q, want_lse=True)     # (units that would be cut in runs are whole then: other roundings)
+    o_tol, l_tol = tree_bound(f64(a["q"]), f64(torch.cat([a["Kc"].view(-1, 128), a["Kd"].view(-1, 128)])),
+                              f64(torch.cat([a["Vc"].view(-1, 128), a["Vd"].view(-1, 128)])), rows + T, 1 / np.sqrt(128))
+    # (either is off by its rounding and the bound; 1.01: the rounding is of the exact value, not of `want`)
+    assert ((got.double() - want.double()).abs() <= 2 * 1.01 * (2.0 ** -8 * want.double().abs() + o_tol)).all()
+    assert ((lse - want_lse).double().abs() <= 2 * 1.01 * (l_tol + 2.0 ** -22 * want_lse.double().abs())).all()
+
+
 @pytest.mark.parametrize("case", [FORMS[0], FORMS[1], FORMS[3], FORMS[5], FORMS[6]])
 def test_tree_waits_that_run_out(case):
     """Copies of the keys that never come: the call ends, says so, and the next one is right again."""
