@@ -198,7 +198,7 @@ def prepare(case, seed):
         s["out"] = torch.zeros(B, T, H, D, dtype=bf, device=dev)
         s["lse"] = torch.zeros(B, H, T, dtype=torch.float32, device=dev)
         s["max_len"] = max(max(x) for x in lens)
-        s["ws"] = torch.empty(48 << 20, dtype=torch.uint8, device=dev)          # one workspace for every call of a program: no call asks for more
+        s["ws"] = torch.empty(32 << 20, dtype=torch.uint8, device=dev)          # one workspace for every call of a program
         return s
     s["len_out"] = torch.empty(B, Hkv, dtype=torch.int32, device=dev)
     if kind == "append":
