@@ -501,13 +501,14 @@ size_t tree_attn_workspace(const lvlm_dims* d) {
 }
 
 #ifdef LVLM_TEST_HOOKS
-static int g_tree_starve = 0;
+static int g_tree_starve = 0, g_tree_stall = 0;
 #endif
 
 }  // namespace lvlm
 
 #ifdef LVLM_TEST_HOOKS
 extern "C" void lvlm_debug_starve_tree(int on) { lvlm::g_tree_starve = on ? 1 : 0; }
+extern "C" void lvlm_debug_stall_tree(int us) { lvlm::g_tree_stall = us; }
 #endif
 
 extern "C" lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void* Vc, const int32_t* table, const int32_t* len,
@@ -572,6 +573,7 @@ extern "C" lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void*
     a.dev_status = dev_status;
 #ifdef LVLM_TEST_HOOKS
     a.starve = g_tree_starve;
+    a.stall = g_tree_stall;
 #endif
     if (L.ctas > 0x7FFFFFFFll) return LVLM_ERR_UNSUPPORTED;
     lvlm_status st;

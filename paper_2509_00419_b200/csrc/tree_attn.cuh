@@ -35,15 +35,20 @@ struct TreeArgs {
     CacheGeom c;
     int32_t* dev_status;
 #ifdef LVLM_TEST_HOOKS
-    int starve;
+    int starve, stall;
 #endif
 };
 
-// The test build can keep the producers from fetching keys, so that waits run out.
+// The test build can keep the producers from fetching keys, so that waits run out, and hold up the warps of half 0 of a tcgen05 CTA
+// for some microseconds before they read what the halves exchange.
 #ifdef LVLM_TEST_HOOKS
 __device__ __forceinline__ bool tree_starved(const TreeArgs& a) { return a.starve != 0; }
+__device__ __forceinline__ void tree_stall(const TreeArgs& a, int half) {
+    for (int i = 0; half == 0 && i < a.stall; ++i) __nanosleep(1000);
+}
 #else
 __device__ __forceinline__ bool tree_starved(const TreeArgs&) { return false; }
+__device__ __forceinline__ void tree_stall(const TreeArgs&, int) {}
 #endif
 
 __device__ __forceinline__ void tree_flag(const TreeArgs& a, int bit) {

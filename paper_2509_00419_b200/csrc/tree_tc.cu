@@ -51,7 +51,10 @@ struct TreeTcSmem {
     uint64_t q_full, k_full[kTStages], k_empty[kTStages], v_full[kTStages], v_empty[kTStages], s_full[2], p_ready[2][2], o_done[2];
     uint32_t tmem_base;
     volatile int abort;
-    float xm[2][kTT], xl[2][kTT];            // one row tile: (max, sum) of a row over the key tiles of either half
+    // One row tile: (max, sum) of a row over the key tiles of either half, in two buffers taken in turn: a half without a key tile in the
+    // next segment waits for nothing there, and stores its own while the other half may still read these.  It comes to the first
+    // buffer again behind the next exchange, which the other half joins only after it has read.
+    float xm[2][2][kTT], xl[2][2][kTT];      // [buffer][half][row]
 };
 
 // Bounded: a wait that runs out sets the status, and the waits after it give up at once.
@@ -497,17 +500,18 @@ tree_tc_kernel(const __grid_constant__ CUtensorMap qmap, const __grid_constant__
             continue;
         }
         if (split) {
-            sm->xm[u][row] = m_used;
-            sm->xl[u][row] = l_row;
+            sm->xm[xc][u][row] = m_used;
+            sm->xl[xc][u][row] = l_row;
             __syncwarp();
             if (lane == 0) mbar_arrive(&sm->x_ready);
             ok = ok && tree_wait(&sm->x_ready, xc, sm, a);
-            xc ^= 1;
-            const float m0 = sm->xm[0][row], m1 = sm->xm[1][row];
+            tree_stall(a, u);
+            const float m0 = sm->xm[xc][0][row], m1 = sm->xm[xc][1][row];
             m_used = fmaxf(m0, m1);
             f0 = m0 > -INFINITY ? ex2_fast(m0 - m_used) : 0.f;
             f1 = m1 > -INFINITY ? ex2_fast(m1 - m_used) : 0.f;
-            l_row = sm->xl[0][row] * f0 + sm->xl[1][row] * f1;
+            l_row = sm->xl[xc][0][row] * f0 + sm->xl[xc][1][row] * f1;
+            xc ^= 1;
             ok = ok && (n_mine == 0 || tree_wait(&sm->o_done[u], (oc >> u) & 1, sm, a));
             ok = ok && ((w.nk + u) / 2 == 0 || tree_wait(&sm->o_done[u ^ 1], (oc >> (u ^ 1)) & 1, sm, a));
         } else {

@@ -761,6 +761,39 @@ def test_tree_waits_that_run_out(case):
     assert same(again, got)
 
 
+def test_runs_with_one_half_held_up():
+    """Units of one row tile in runs, heads of two and of one key tile in turn: the half that has no key tile in the next unit is through
+    with it, as far as it may go, before the other has read what the halves exchanged for this one."""
+    r = np.random.default_rng(32)
+    B, H, Hkv, T, page = 25, 32, 8, 13, 64
+    q, Kp, Vp = bf(r, B, T, H, 128).cuda(), bf(r, B * Hkv * 4, page, 128).cuda(), bf(r, B * Hkv * 4, page, 128).cuda()
+    tab = torch.full((B, Hkv, 150), -1, dtype=torch.int32, device="cuda")
+    tab[:, :, :4] = dev(r.permutation(B * Hkv * 4).reshape(B, Hkv, 4))
+    rows = np.where(np.arange(B * Hkv) % 2 == 0, 250, 100).reshape(B, Hkv)
+    a = dict(q=q, Kc=Kp, Vc=Vp, length=dev(rows), table=tab)           # (a capacity of 9600: runs)
+    j = torch.arange(256, device="cuda")
+    at = tab[:, :, j // page].long() * page + j % page
+    K, V = (x.view(-1, 128)[at].double().repeat_interleave(H // Hkv, 1) for x in (Kp, Vp))
+    x = torch.einsum("bthd,bhnd->bhtn", q.double(), K) / 128 ** 0.5
+    x.masked_fill_((j >= dev(rows)[..., None]).repeat_interleave(H // Hkv, 1)[:, :, None], -torch.inf)
+    want, want_lse = torch.einsum("bhtn,bhnd->bthd", torch.softmax(x, -1), V), torch.logsumexp(x, -1)
+    o_tol, l_tol = tree_bound(f64(q), f64(K), f64(V), 256, 1 / np.sqrt(128))
+    assert count_launches(lambda: L.tree_attn(**a)) == 2
+    try:
+        L.use_library(BU.build_test())
+        L.lib().lvlm_debug_stall_tree(50)
+        st = flag()
+        got, lse = L.tree_attn(**a, want_lse=True, dev_status=st)
+        torch.cuda.synchronize()
+        assert st.item() == 0
+    finally:
+        L.lib().lvlm_debug_stall_tree(0)
+        L.use_library(None)
+    assert ((got.double() - want).abs() <= 2.0 ** -8 * want.abs() + o_tol).all()
+    assert ((lse.double() - want_lse).abs() <= l_tol + 2.0 ** -22 * want_lse.abs()).all()
+    assert same(L.tree_attn(**a)[0], got)
+
+
 def test_lengths_grow_where_they_lie():
     """One token a call into a paged cache, the length read and written by the same kernel, forty times over."""
     r = np.random.default_rng(31)
