@@ -326,6 +326,10 @@ __global__ void __launch_bounds__(kTreeCombineWarps * 32) tree_combine_kernel(co
     int2 of;                                                    // first slot and how many more parts
     if (RUNS) {
         of = a.part_of[blockIdx.x];
+        if (of.x >= 0 && !tree_record(of.x, of.y)) {            // (uniform over the block, like all that ends it here)
+            if (threadIdx.x == 0) tree_flag(a, LVLM_DEV_TIMEOUT);
+            return;
+        }
     } else {
         const int step = tree_part(h, a.S);
         of = make_int2(step >= h.nt ? -1 : hd * a.S * a.units + unit, (h.nt - 1) / step);
@@ -508,6 +512,7 @@ static int g_tree_starve = 0, g_tree_stall = 0;
 
 #ifdef LVLM_TEST_HOOKS
 extern "C" void lvlm_debug_starve_tree(int on) { lvlm::g_tree_starve = on ? 1 : 0; }
+extern "C" int lvlm_debug_tree_record(int first, int more) { return lvlm::tree_record(first, more); }
 extern "C" void lvlm_debug_stall_tree(int us) { lvlm::g_tree_stall = us; }
 #endif
 

@@ -69,6 +69,10 @@ __device__ __forceinline__ TreeHead tree_head(const TreeArgs& a, int hd, int key
 // Steps in a part of a unit.
 __device__ __forceinline__ int tree_part(const TreeHead& h, int S) { return S == 1 ? max(h.nt, 1) : max(1, (h.nt + S - 1) / S); }
 
+// Whether a record of part_of names CTAs that there are: the one that begins the unit, and at least one that goes on with it.  A scheduler
+// that gave up on a wait leaves the records behind it as the workspace held them.
+__host__ __device__ inline bool tree_record(int first, int more) { return first >= 0 && more > 0 && more < kTreeTcCtas - first; }
+
 // Word w of what draft t sees, limited to the n drafts there are.
 __device__ __forceinline__ uint32_t tree_see(const TreeArgs& a, int b, int t, int n, int w) {
     const int u0 = w * 32;

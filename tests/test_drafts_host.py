@@ -206,6 +206,19 @@ def test_tree_workspace_never_shrinks(lib, heads):
             assert sizes[i] >= sizes[i - 1], (line[i - 1], line[i])
 
 
+def test_records_of_cut_units():
+    """Any two words that a workspace may hold: what is taken for a record names CTAs of the grid only."""
+    t = ctypes.CDLL(B.build_test())
+    ok = lambda first, more: bool(t.lvlm_debug_tree_record(ctypes.c_int(first), ctypes.c_int(more)))
+    for first in range(-2, 150):
+        for more in range(-2, 150):
+            assert ok(first, more) == (0 <= first and 0 < more and first + more <= 147), (first, more)
+    far = [-(1 << 31), (1 << 31) - 1, 0x7F7F7F7F, -0x7F7F7F7F, 1 << 30, 148, 147, 1, 0, -1]
+    for x in far:
+        for y in far:
+            assert ok(x, y) == (0 <= x and 0 < y and x + y <= 147), (x, y)
+
+
 def test_tree_workspace_is_small(lib):
     """The widest trees over the longest caches fit 32 MiB, a token over a short cache asks for little."""
     for H, Hkv in ((8, 8), (28, 4), (32, 8), (48, 8), (64, 1)):

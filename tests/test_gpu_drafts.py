@@ -761,6 +761,34 @@ def test_tree_waits_that_run_out(case):
     assert same(again, got)
 
 
+@pytest.mark.parametrize("fill", [0x00, 0x7F, 0xFF, 0x01])
+def test_tree_waits_that_run_out_in_long_runs(fill):
+    """Runs of more segments than a scheduler is ahead: it gives up with records of cut units not written, whatever lies in their place."""
+    r = np.random.default_rng(33)
+    B, H, Hkv, T, page = 25, 32, 8, 13, 64
+    rows = np.where(r.random((B, Hkv)) < 0.93, r.integers(0, 60, size=(B, Hkv)), 9000)
+    mp = 141
+    q, Kp, Vp = bf(r, B, T, H, 128).cuda(), bf(r, 64, page, 128).cuda(), bf(r, 64, page, 128).cuda()
+    tab = torch.full((B, Hkv, 150), -1, dtype=torch.int32, device="cuda")
+    tab[:, :, :mp] = dev(r.integers(0, 64, size=(B, Hkv, mp)))         # (pages that heads share)
+    a = dict(q=q, Kc=Kp, Vc=Vp, length=dev(rows), table=tab)
+    assert count_launches(lambda: L.tree_attn(**a)) == 2
+    want, _ = L.tree_attn(**a)
+    ws = torch.full((L.workspace_bytes(L.OP_TREE_ATTN, L.tree_dims(q, Kp, tab)),), fill, dtype=torch.uint8, device="cuda")
+    try:
+        L.use_library(BU.build_test())
+        st = flag()
+        L.lib().lvlm_debug_starve_tree(1)
+        L.tree_attn(**a, ws=ws, dev_status=st)
+        torch.cuda.synchronize()
+        assert st.item() & L.DEV_TIMEOUT
+    finally:
+        L.lib().lvlm_debug_starve_tree(0)
+        L.use_library(None)
+    st = flag()
+    assert same(L.tree_attn(**a, ws=ws, dev_status=st)[0], want) and st.item() == 0
+
+
 def test_runs_with_one_half_held_up():
     """Units of one row tile in runs, heads of two and of one key tile in turn: the half that has no key tile in the next unit is through
     with it, as far as it may go, before the other has read what the halves exchanged for this one."""
