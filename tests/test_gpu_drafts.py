@@ -105,6 +105,15 @@ def test_rope_append(B, H, Hkv, T, cap, page, rot, interleaved, sections, inplac
         assert torch.isnan(Kd[other]).all() and torch.isnan(Vd[other]).all()
 
 
+# more tokens than the few that get a large CTA each (296): another instance of the kernel
+@pytest.mark.parametrize("B,H,Hkv,T,cap,page,rot,interleaved,sections,inplace", [
+    (1, 4, 2, 296, 300, 0, 128, False, None, True), (1, 4, 2, 297, 320, 16, 128, False, None, True), (2, 28, 4, 200, 512, 16, 128, False, (16, 24, 24), True),
+    (1, 48, 8, 333, 350, 0, 64, True, None, False), (3, 8, 2, 150, 256, 64, 112, False, (0, 56, 0), True), (1, 8, 8, 301, 320, 32, 128, True, (20, 21, 23), False),
+    (298, 2, 1, 1, 48, 16, 128, False, None, True), (5, 7, 1, 120, 128, 128, 0, False, None, False)])
+def test_rope_append_of_prompts(B, H, Hkv, T, cap, page, rot, interleaved, sections, inplace):
+    test_rope_append(B, H, Hkv, T, cap, page, rot, interleaved, sections, inplace)
+
+
 def test_rope_append_into_a_draft_cache_without_queries():
     r = np.random.default_rng(7)
     kn, vn = bf(r, 2, 6, 3, 128), bf(r, 2, 6, 3, 128)
