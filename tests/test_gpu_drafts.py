@@ -395,6 +395,67 @@ def test_tree_attn_shared_mask_large_logits_no_drafts():
     run_tree(2, 8, 2, 12, [50, 9, 70, 100], [12, 5], 64, "any", seed=3, fill=float("inf"))
 
 
+@pytest.mark.parametrize("B,H,Hkv,T,page,shared,max_len", [
+    (3, 4, 2, 1, 16, 48, None), (3, 8, 2, 5, 64, 192, None), (2, 8, 1, 40, 32, 128, None), (2, 8, 1, 40, 64, 640, 30000), (160, 1, 1, 40, 16, 16, 20000)])
+def test_pages_shared_by_sequences(B, H, Hkv, T, page, shared, max_len):
+    """A prompt that all sequences begin with lies in pages that their tables share; what they append lies in pages of their own."""
+    r = np.random.default_rng(B + T)
+    own, cap = 2 * page, shared + 2 * page
+    K, V = bf(r, 1, Hkv, shared, 128), bf(r, 1, Hkv, shared, 128)
+    first = shared // page
+    n_pages = Hkv * first + B * Hkv * 2 + 1
+    place = r.permutation(n_pages)
+    head = np.broadcast_to(place[:Hkv * first].reshape(1, Hkv, first), (B, Hkv, first))
+    table = np.concatenate([head, place[Hkv * first:Hkv * first + B * Hkv * 2].reshape(B, Hkv, 2)], 2)
+    wide = np.concatenate([table, np.full((B, Hkv, (max_len or 0) // page), -1)], 2)      # (a capacity for the length expected)
+    Kp, Vp = (torch.full((n_pages, page, 128), float("nan"), dtype=BF) for _ in range(2))
+    at = torch.from_numpy(head[0].copy())
+    Kp[at.reshape(-1)], Vp[at.reshape(-1)] = K[0].reshape(-1, page, 128), V[0].reshape(-1, page, 128)
+    Kp, Vp, tab = Kp.cuda(), Vp.cuda(), dev(wide)
+    n_new = own - 3
+    kn, vn = bf(r, B, n_new, Hkv, 128), bf(r, B, n_new, Hkv, 128)
+    count = r.integers(0, n_new + 1, size=B)
+    ln, st = torch.full((B, Hkv), shared, dtype=torch.int32, device="cuda"), flag()
+    L.rope_append(kn.cuda(), vn.cuda(), None, None, Kp, Vp, ln, table=tab, count=dev(count), dev_status=st)
+    Kw, Vw = np.zeros((B, Hkv, cap, 128)), np.zeros((B, Hkv, cap, 128))
+    Kw[:, :, :shared], Vw[:, :, :shared] = f64(K), f64(V)
+    Kw, Vw, want_len = DO.append(Kw, Vw, np.full((B, Hkv), shared), f64(kn), f64(vn), count)
+    assert st.item() == 0 and np.array_equal(i32(ln), want_len)
+    assert same(Kp[at.reshape(-1)], K[0].reshape(-1, page, 128)) and same(Vp[at.reshape(-1)], V[0].reshape(-1, page, 128))
+    q, Kd, Vd = bf(r, B, T, H, 128), bf(r, B, Hkv, T, 128), bf(r, B, Hkv, T, 128)
+    got, _ = L.tree_attn(q.cuda(), Kp, Vp, ln, Kd=Kd.cuda(), Vd=Vd.cuda(), table=tab, max_len=max_len, dev_status=st)
+    see = np.tril(np.ones((T, T), bool))[None].repeat(B, 0)
+    want, _ = DO.tree_attn(f64(q), Kw, Vw, want_len, f64(Kd), f64(Vd), see, [T] * B)
+    tol, _ = tree_bound(f64(q), np.concatenate([Kw, f64(Kd)], 2), np.concatenate([Vw, f64(Vd)], 2), cap + T, 1 / np.sqrt(128))
+    assert st.item() == 0 and (np.abs(f64(got) - want) <= 2.0 ** -8 * np.abs(want) + tol).all()
+
+
+@pytest.mark.parametrize("T,B", [(1, 20), (17, 20), (40, 20), (40, 200)])
+def test_probabilities_keep_sixteen_bits(T, B):
+    """Two keys, logits 0 and -x, values -bf16(p) v and v with p = exp(-x): the result is v (p - bf16(p)) / (1 + p), nothing but what the
+    first bf16 part of p leaves.  Off by: the logit, whose one product is exact, and its scale, 2^-24 a factor and a rounding, four of
+    them of x log2(e) < 4.4 (2^-20); the exponential, 2^-22; the second part, 2^-8 of at most 2^-8 of p <= 1; three sums, 2^-23 each:
+    below 2^-15 v in all.  Beside it the result's own rounding."""
+    r = np.random.default_rng(T)
+    x = r.uniform(0.05, 3.0, size=(B, 4))
+    q, K, V = torch.zeros(B, T, 4, 128), torch.zeros(B, 4, 2, 128), torch.zeros(B, 4, 2, 128)
+    q[..., 0] = 8.0
+    K[:, :, 1, 0] = -torch.from_numpy(x * np.sqrt(128) / 8).float()
+    K = K.to(BF)
+    p = np.exp(f64(K)[:, :, 1, 0] * 8 / np.sqrt(128))                 # of the key as it was rounded
+    v = 2.0 ** (np.arange(128) % 4)
+    V[:, :, 1] = torch.from_numpy(v).float()
+    V[:, :, 0] = -torch.from_numpy(p).to(BF).float()[..., None] * V[:, :, 1]
+    V = V.to(BF)
+    want = (f64(V)[:, :, 0] + p[..., None] * f64(V)[:, :, 1]) / (1 + p[..., None])
+    assert (np.abs(want) > 2 * 2.0 ** -15 * v).mean() > 0.5           # without the second part the result would be 0, and refused below
+    ln = torch.full((B, 4), 2, dtype=torch.int32, device="cuda")
+    got, lse = L.tree_attn(q.to(BF).cuda(), K.cuda(), V.cuda(), ln, want_lse=True, max_len=2)
+    err = np.abs(f64(got).transpose(0, 2, 1, 3) - want[:, :, None]) - 2.0 ** -8 * np.abs(want[:, :, None])
+    assert (err <= 2.0 ** -15 * v).all()
+    assert (np.abs(f64(lse) - np.log1p(p)[..., None]) <= 2.0 ** -20).all()
+
+
 @pytest.mark.parametrize("T", [3, 60])
 def test_tree_attn_flags(T):
     """A bad length, count or page number: flagged, nothing outside is read, the other heads are as without it."""
