@@ -392,7 +392,8 @@ lvlm_status lvlm_commit_rows(const void* Kd, const void* Vd, const int32_t* inde
  *   lse[b,h,t]     = natural log of the sum of the exponentials of the scaled logits
  * A row that sees nothing gives out = 0 and lse = -inf.  With one draft a sequence this is decode attention over either kind
  * of cache.
- *   q        [B][T][H][D] bf16 (strides d->q_stride_*)     out  [B][T][H][D] bf16, packed
+ *   q        [B][T][H][D] bf16 (strides d->q_stride_*)     out  [B][T][H][D] bf16, packed; q itself where q is packed, any other
+ *                                                          overlap with q is INVALID_ARG
  *   len      [B][Hkv] int32                                lse  optional [B][H][T] fp32
  *   Kd, Vd   [B][Hkv][draft_cap][D] bf16, the drafts' keys (rotated) and values, or both NULL: only the cache is seen
  *   mask     [B][T][(T+31)/32] uint32 ([T][(T+31)/32] with d->mask_shared): bit u % 32 of word u / 32 of row t set = t sees

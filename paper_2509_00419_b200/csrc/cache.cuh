@@ -38,6 +38,12 @@ inline lvlm_status cache_geom(const lvlm_dims* d, const int32_t* table, CacheGeo
     return c->sh % 8 || c->sb % 8 ? LVLM_ERR_ALIGNMENT : LVLM_OK;
 }
 
+// Host: whether the np bytes from p and the nq bytes from q share some.
+inline bool overlap(const void* p, int64_t np, const void* q, int64_t nq) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
+    return a < b + (uintptr_t)nq && b < a + (uintptr_t)np;
+}
+
 // Device: element offset of row `row` (0 <= row < cap) of head hd = b * Hkv + g, or -1: its page number is not one of the pool.
 __device__ __forceinline__ int64_t cache_row(const CacheGeom& c, const int32_t* table, int b, int g, int row) {
     if (!c.page) return (int64_t)b * c.sb + (int64_t)g * c.sh + (int64_t)row * kHeadDim;

@@ -238,12 +238,6 @@ __global__ void __launch_bounds__(kCommitThreads, 8) commit_rows_kernel(const Co
     }
 }
 
-// Bytes [p, p + n elements) and [q, ...) share some.
-static bool overlap(const void* p, int64_t np, const void* q, int64_t nq) {
-    const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = reinterpret_cast<uintptr_t>(q);
-    return a < b + (uintptr_t)nq * 2 && b < a + (uintptr_t)np * 2;
-}
-
 static lvlm_status grow_len(int32_t* len, const int32_t* count, int count_heads, int heads, const CacheGeom& c, int T, cudaStream_t stream) {
     return launch_kernel(grow_len_kernel, dim3((unsigned)((heads + 255) / 256)), dim3(256), 0, stream, 1, len, count, count_heads, heads,
                          c.Hkv, T, c.cap);
@@ -279,7 +273,7 @@ extern "C" lvlm_status lvlm_rope_append(const void* q, const void* k_new, const 
         a.q_sh % 8 || a.q_sn % 8 || a.q_sb % 8 || a.n_sh % 8 || a.n_sn % 8 || a.n_sb % 8)
         return LVLM_ERR_ALIGNMENT;
     if (q && q_out != q &&
-        overlap(q, (d->B - 1) * a.q_sb + (d->T - 1) * a.q_sn + (d->H - 1) * a.q_sh + kHeadDim, q_out, (int64_t)d->B * a.qo_sb))
+        overlap(q, 2 * ((d->B - 1) * a.q_sb + (d->T - 1) * a.q_sn + (d->H - 1) * a.q_sh + kHeadDim), q_out, 2 * d->B * a.qo_sb))
         return LVLM_ERR_INVALID_ARG;
     const int64_t tokens = (int64_t)d->B * d->T, heads = (int64_t)d->B * d->Hkv;
     if (tokens > 0x7FFFFFFFll || heads > 0x7FFFFFFFll) return LVLM_ERR_UNSUPPORTED;

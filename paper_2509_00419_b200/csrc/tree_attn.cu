@@ -537,6 +537,11 @@ extern "C" lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void*
     if (!aligned16(q) || !aligned16(Kc) || !aligned16(Vc) || !aligned16(Kd) || !aligned16(Vd) || !aligned16(out) || a.q_sh % 8 ||
         a.q_sn % 8 || a.q_sb % 8 || d_sh % 8 || d_sb % 8)
         return LVLM_ERR_ALIGNMENT;
+    // Queries may be overwritten where a row's result takes its own query's place; anywhere else CTAs may still have to read them.
+    const int64_t packed_n = (int64_t)d->H * d->D, packed_b = d->T * packed_n;
+    if (out == q ? (d->H > 1 && a.q_sh != d->D) || (d->T > 1 && a.q_sn != packed_n) || (d->B > 1 && a.q_sb != packed_b)
+                 : overlap(q, 2 * ((d->B - 1) * a.q_sb + (d->T - 1) * a.q_sn + (d->H - 1) * a.q_sh + kHeadDim), out, 2 * d->B * packed_b))
+        return LVLM_ERR_INVALID_ARG;
     TreeLayout L;
     if (!tree_layout(d, a.c.cap, &L)) return LVLM_ERR_INVALID_ARG;
     // In runs a part lies in `out` while other CTAs may still fetch the queries of its unit: where out is q, units go in waves.

@@ -188,6 +188,22 @@ def test_tree_attn_refusals(lib):
     assert L.workspace_bytes(L.OP_TREE_ATTN, _dims(T=0)) == 0
 
 
+def test_tree_attn_refuses_results_over_other_queries(lib):
+    """out is q, row for row, or lies elsewhere."""
+    def call(d, q=P, out=P):
+        return lib.lvlm_tree_attn(q, P2, P2, None, P, None, None, None, None, ctypes.byref(d), ctypes.c_float(0.1), out, None, None, 0, None, None)
+
+    at = lambda n: ctypes.c_void_p(0x100000 + n)
+    size = 2 * 5 * 8 * 128 * 2
+    split = _dims(cap=5000)                                                           # (refused for its workspace where nothing else is wrong)
+    for n in (16, 256, size - 16):
+        assert call(split, out=at(n)) == call(split, q=at(n)) == L.ERR_INVALID_ARG, n
+    assert call(split) == call(split, out=at(size)) == call(split, q=at(size)) == L.ERR_WORKSPACE
+    for kw in (dict(q_stride_n=9 * 128), dict(q_stride_b=6 * 8 * 128), dict(q_stride_h=256)):
+        assert call(_dims(cap=5000, **kw)) == L.ERR_INVALID_ARG, kw
+    assert call(_dims(cap=5000, q_stride_n=9 * 128), out=at(2 * 5 * 9 * 128 * 2)) == L.ERR_WORKSPACE
+
+
 # a program sizes a workspace once, for its widest batch, longest cache and largest tree: nothing smaller may ask for more
 @pytest.mark.parametrize("heads", [(8, 8), (28, 4), (32, 8), (48, 8), (1, 1), (64, 1)])
 def test_tree_workspace_never_shrinks(lib, heads):
