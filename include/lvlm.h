@@ -354,7 +354,8 @@ lvlm_status lvlm_decode_attn_static(const void* q, void* Kc, void* Vc, int32_t* 
  *              channels that follow it as they are
  *   cos_sin    [n_pos][rot] fp32, 16-byte aligned; cos_sin and pos are only needed with rot > 0
  *   len        [B][Hkv] int32, or NULL: all zero (a draft cache)
- *   len_out    optional [B][Hkv] int32, may be len itself (a second small launch then where T > 1)
+ *   len_out    optional [B][Hkv] int32, may be len itself (a second small launch then where T > 1); any other overlap with len,
+ *              or with count, is INVALID_ARG (count may be both of them in one)
  *   acc_score  optional [B][Hkv][cap] fp32: the new entries become 0, as lvlm_decode_attn starts them
  *   pos_cache  optional [B][Hkv][cap] int32: the new entries take pos (of axis 0); needs pos
  * Reads d: B,H,Hkv,D,T,rot,interleaved,n_pos,axes,sect0,sect1,q_stride_*,new_stride_*, and the cache's fields.

@@ -238,6 +238,14 @@ __global__ void __launch_bounds__(kCommitThreads, 8) commit_rows_kernel(const Co
     }
 }
 
+// Whether len_out [heads] lies over lengths or counts that other threads may still have to read: over len or count [counts] other than
+// place for place (count only where len_out is len: the thread that writes such a length has read both).
+static bool lengths_clash(const int32_t* len, const int32_t* len_out, int64_t heads, const int32_t* count, int64_t counts) {
+    if (!len_out) return false;
+    if (len && len != len_out && overlap(len, heads * 4, len_out, heads * 4)) return true;
+    return count && overlap(count, counts * 4, len_out, heads * 4) && !(len == len_out && count == len_out && counts == heads);
+}
+
 static lvlm_status grow_len(int32_t* len, const int32_t* count, int count_heads, int heads, const CacheGeom& c, int T, cudaStream_t stream) {
     return launch_kernel(grow_len_kernel, dim3((unsigned)((heads + 255) / 256)), dim3(256), 0, stream, 1, len, count, count_heads, heads,
                          c.Hkv, T, c.cap);
@@ -277,6 +285,7 @@ extern "C" lvlm_status lvlm_rope_append(const void* q, const void* k_new, const 
         return LVLM_ERR_INVALID_ARG;
     const int64_t tokens = (int64_t)d->B * d->T, heads = (int64_t)d->B * d->Hkv;
     if (tokens > 0x7FFFFFFFll || heads > 0x7FFFFFFFll) return LVLM_ERR_UNSUPPORTED;
+    if (lengths_clash(len, len_out, heads, count, d->B)) return LVLM_ERR_INVALID_ARG;
     a.q = static_cast<const __nv_bfloat16*>(q);
     a.k_new = static_cast<const __nv_bfloat16*>(k_new);
     a.v_new = static_cast<const __nv_bfloat16*>(v_new);
@@ -313,6 +322,7 @@ extern "C" lvlm_status lvlm_commit_rows(const void* Kd, const void* Vd, const in
     if (!aligned16(Kd) || !aligned16(Vd) || !aligned16(Kc) || !aligned16(Vc) || a.d_sh % 8 || a.d_sb % 8) return LVLM_ERR_ALIGNMENT;
     const int64_t heads = (int64_t)d->B * d->Hkv, runs = ((int64_t)d->T + kCommitRows - 1) / kCommitRows;
     if (heads > 0x7FFFFFFFll || runs > 65535) return LVLM_ERR_UNSUPPORTED;
+    if (lengths_clash(len, len_out, heads, count, d->count_heads ? heads : d->B)) return LVLM_ERR_INVALID_ARG;
     a.Kd = static_cast<const __nv_bfloat16*>(Kd);
     a.Vd = static_cast<const __nv_bfloat16*>(Vd);
     a.index = index; a.count = count; a.pos = pos;

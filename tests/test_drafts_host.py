@@ -188,6 +188,27 @@ def test_tree_attn_refusals(lib):
     assert L.workspace_bytes(L.OP_TREE_ATTN, _dims(T=0)) == 0
 
 
+def test_appends_refuse_lengths_over_what_others_read(lib):
+    """len_out is len, or shares nothing with len or count: only then has every thread read what another writes."""
+    at = lambda n: ctypes.c_void_p(0x9100000 + n)
+
+    def append(ln, lo, count, **kw):
+        return lib.lvlm_rope_append(None, P, P, None, None, count, None, P2, P2, None, ln, lo, None, None, ctypes.byref(_dims(rot=0, **kw)), None, None)
+
+    def commit(ln, lo, count, **kw):
+        return lib.lvlm_commit_rows(P, P, P, count, None, P2, P2, None, ln, lo, None, None, ctypes.byref(_dims(**kw)), None, None)
+
+    for call in (append, commit):                                    # two sequences of two heads: 16 bytes of lengths, 8 of counts
+        for n in (4, 8, 12, -4, -12):
+            assert call(at(0), at(n), None) == L.ERR_INVALID_ARG, n
+        for n in (0, 4, 8, 12, -4):
+            assert call(at(64), at(0), at(n)) == call(at(0), at(0), at(n)) == call(None, at(0), at(n)) == L.ERR_INVALID_ARG, n
+    for n in (4, 12, -12):
+        assert commit(at(0), at(0), at(n), count_heads=1) == L.ERR_INVALID_ARG
+    assert commit(at(64), at(0), at(0), count_heads=1) == L.ERR_INVALID_ARG
+    assert append(at(64), at(0), at(0), Hkv=1) == L.ERR_INVALID_ARG
+
+
 def test_tree_attn_refuses_results_over_other_queries(lib):
     """out is q, row for row, or lies elsewhere."""
     def call(d, q=P, out=P):

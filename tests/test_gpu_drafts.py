@@ -227,6 +227,18 @@ def test_commit_moves_a_ragged_cache(rows, page):
     assert np.array_equal(f64(Kl), want[0]) and np.array_equal(f64(Vl), want[1])
 
 
+@pytest.mark.parametrize("rows", [20, 100])
+def test_commit_by_the_lengths_themselves(rows):
+    """count and length in one tensor: every head doubles."""
+    r = np.random.default_rng(rows)
+    Kd, Vd, K, V = bf(r, 2, 3, rows, 128), bf(r, 2, 3, rows, 128), bf(r, 2, 3, 2 * rows, 128), bf(r, 2, 3, 2 * rows, 128)
+    ln = r.integers(0, rows + 1, size=(2, 3))
+    want = DO.commit(f64(K), f64(V), ln, f64(Kd), f64(Vd), None, ln)
+    Kc, Vc, ld, st = K.cuda(), V.cuda(), dev(ln), flag()
+    L.commit_rows(Kd.cuda(), Vd.cuda(), Kc, Vc, ld, ld, dev_status=st)
+    assert st.item() == 0 and np.array_equal(i32(ld), 2 * ln) and np.array_equal(f64(Kc), want[0]) and np.array_equal(f64(Vc), want[1])
+
+
 def test_commit_flags():
     r = np.random.default_rng(11)
     B, Hkv, T = 4, 2, 5
