@@ -407,7 +407,7 @@ lvlm_status lvlm_commit_rows(const void* Kd, const void* Vd, const int32_t* inde
  * it, and one that splits nothing takes ws = NULL.  Calls that may overlap on the GPU need workspaces of their own.
  * Reads d: B,H,Hkv,D,N,T,draft_cap,mask_shared,q_stride_*,draft_stride_*, and the cache's fields.
  * Errors: INVALID_ARG (NULL q/Kc/Vc/len/out, one of Kd/Vd, a mask without drafts, draft_cap < T, scale <= 0), UNSUPPORTED
- * (D != 128, T > 256, H/Hkv > 64), ALIGNMENT, WORKSPACE.  Contents of out and lse are undefined when a kernel gave up on a
+ * (D != 128, T > 256, H/Hkv > 64, cap / 128 x tiles of 128 query rows > 2^30), ALIGNMENT, WORKSPACE.  Contents of out and lse are undefined when a kernel gave up on a
  * wait and set LVLM_DEV_TIMEOUT.
  */
 lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void* Vc, const int32_t* table, const int32_t* len,

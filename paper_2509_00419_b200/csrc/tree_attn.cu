@@ -418,7 +418,7 @@ static int tree_unit_tiles(int64_t heads, int tiles, int64_t keys) {
 // How a call is carried out.  `need` is what this form uses, `total` what a caller is told: at least what any problem that is no larger
 // uses, so that it never shrinks as a problem grows.
 struct TreeLayout {
-    int tc, R, runs, S, unit_tiles, units, pitch;
+    int tc, R, runs, S, tiles, unit_tiles, units, pitch;
     int64_t ctas;
     size_t off_o, off_lo, off_of, need, total;
 };
@@ -478,6 +478,7 @@ static bool tree_layout(const lvlm_dims* d, int64_t cap, TreeLayout* L) {
     L->tc = R > 2 || d->T > 32 * kTreeMmaWords || tc_us < mma_us;
     L->R = R;
     L->S = L->tc ? (int)parts : S;
+    L->tiles = tiles;
     L->unit_tiles = unit_tiles;
     L->units = tc_units;
     L->pitch = unit_tiles * kTreeTcRows;
@@ -544,6 +545,7 @@ extern "C" lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void*
         return LVLM_ERR_INVALID_ARG;
     TreeLayout L;
     if (!tree_layout(d, a.c.cap, &L)) return LVLM_ERR_INVALID_ARG;
+    if (((int64_t)a.c.cap / kTreeTcRows + 3) * L.tiles > 0x3FFFFFFF) return LVLM_ERR_UNSUPPORTED;     // (tree_weight)
     // In runs a part lies in `out` while other CTAs may still fetch the queries of its unit: where out is q, units go in waves.
     if (L.runs && out == q) {
         if ((int64_t)d->B * d->Hkv > 65535) return LVLM_ERR_INVALID_ARG;

@@ -70,8 +70,8 @@ __device__ __forceinline__ bool tree_wait(uint64_t* bar, uint32_t parity, TreeTc
 // Halves of two words in one: their lower ones (selector 0x5410) or their upper ones (0x7632).
 __device__ __forceinline__ uint32_t halves(float x, float y, uint32_t selector) { return __byte_perm(__float_as_uint(x), __float_as_uint(y), selector); }
 
-// Row tiles of a head that are asked for, and what it weighs: a pair of them 2 a key tile, an odd one 1 (far below 2^31: a tile is
-// 64 KB); a head without keys one tile, so that its rows are written.
+// Row tiles of a head that are asked for, and what it weighs: a pair of them 2 a key tile, an odd one 1 (at most 2^30: a capacity
+// that would give more, in pages that lie in a table many times, is refused); a head without keys one tile, so that its rows are written.
 __device__ __forceinline__ int tree_rt(const TreeHead& h, int tt) { return h.n <= tt ? (h.n > 0) : (h.n + tt - 1) / tt; }
 __device__ __forceinline__ int tree_weight(const TreeHead& h, int tt) { return max(h.nt, 1) * tree_rt(h, tt); }
 

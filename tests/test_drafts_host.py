@@ -209,6 +209,15 @@ def test_appends_refuse_lengths_over_what_others_read(lib):
     assert append(at(64), at(0), at(0), Hkv=1) == L.ERR_INVALID_ARG
 
 
+def test_tree_attn_refuses_more_tiles_than_it_can_count(lib):
+    """128 row tiles a head (64 query heads of 256 drafts) over 2^31 rows, in a few large pages that lie in the table many times."""
+    def call(max_pages):
+        d = _dims(B=1, H=64, Hkv=1, T=256, page=1 << 20, n_pages=4, max_pages=max_pages)
+        return lib.lvlm_tree_attn(P, P2, P2, P, P, None, None, None, None, ctypes.byref(d), ctypes.c_float(0.1), P2, None, ctypes.c_void_p(8), 8, None, None)
+
+    assert call(2047) == call(1025) == L.ERR_UNSUPPORTED
+
+
 def test_tree_attn_refuses_results_over_other_queries(lib):
     """out is q, row for row, or lies elsewhere."""
     def call(d, q=P, out=P):
