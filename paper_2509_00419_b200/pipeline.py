@@ -197,6 +197,7 @@ class PagedLayers:
         self.V = torch.empty(n_pages, page, 128, dtype=bf, device=device)
         self.table = torch.full((n_layers, B, Hkv, max_pages), -1, dtype=i32, device=device)
         self.len = torch.zeros(n_layers, B, Hkv, dtype=i32, device=device)
+        self.room = torch.zeros(n_layers, B, Hkv, dtype=i32, device=device)      # rows that the pages of a head hold
         self.Kd = torch.empty(n_layers, B, Hkv, T, 128, dtype=bf, device=device)
         self.Vd = torch.empty(n_layers, B, Hkv, T, 128, dtype=bf, device=device)
         self.q = torch.empty(B, T, H, 128, dtype=bf, device=device)
@@ -221,6 +222,7 @@ class PagedLayers:
                 self._table[l, b, g, j] = self._free.pop()
         self._held = torch.maximum(self._held, need)
         self.table.copy_(self._table)
+        self.room.copy_(self._held * self.page)
 
     def release(self, b: int):
         """Sequence ``b`` is finished: its pages are free again and its lengths 0.  Calls before this one in the stream still see them."""
@@ -231,6 +233,7 @@ class PagedLayers:
         held.fill_(-1)
         self._held[:, b] = 0
         self.table[:, b].copy_(held)
+        self.room[:, b].zero_()
         self.len[:, b].zero_()
 
     def pages_free(self) -> int:
@@ -254,10 +257,23 @@ class PagedLayers:
         return out
 
     def commit(self, index, count):
-        """Appends the drafts index [B][T] (the accepted path), ``count`` [B] of them, to the caches of all layers."""
+        """Appends the drafts index [B][T] (the accepted path), ``count`` [B] of them, to the caches of all layers.  A sequence with a
+        head that has no pages for them is left as it was, in all layers, and the status takes DEV_BOUNDS: after ``reserve`` it can be
+        committed again, with a count of 0 for the others."""
         shp = (self.nl * self.B, self.Hkv)
+        fits = (self.len + count[:, None] <= self.room).all(2).all(0)
+        count = torch.where(fits, count, -1)                               # (a count that is none: flagged and skipped)
         L.commit_rows(self.Kd.view(*shp, self.T, 128), self.Vd.view(*shp, self.T, 128), self.K, self.V, self.len.view(shp),
                       count.repeat(self.nl), index=index.repeat(self.nl, 1), table=self.table.view(*shp, -1), dev_status=self.status)
+
+    def check(self):
+        """Raises if a call since the last check left something out or gave up.  Reads the status back."""
+        status = int(self.status.item())
+        self.status.zero_()
+        if status:
+            said = [text for bit, text in ((L.DEV_TIMEOUT, "a kernel gave up on a wait"),
+                                           (L.DEV_BOUNDS, "a length, count, position or page was out of bounds, or a commit had no pages")) if status & bit]
+            raise RuntimeError("; ".join(said) or f"device status {status}")
 
 
 def capture(fn, warmup=1):

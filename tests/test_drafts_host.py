@@ -265,6 +265,25 @@ def test_records_of_cut_units():
             assert ok(x, y) == (0 <= x and 0 < y and x + y <= 147), (x, y)
 
 
+def test_room_follows_the_pages():
+    """What the commits are held against: the rows of the pages that a head has."""
+    from paper_2509_00419_b200.pipeline import PagedLayers
+
+    c = PagedLayers(2, 2, 4, 2, n_pages=20, page=16, max_pages=3, T=4, device="cpu")
+    rows = torch.tensor([[[17, 0], [16, 48]], [[1, 33], [32, 5]]])
+    c.reserve(rows)
+    assert torch.equal(c.room.long(), (rows + 15) // 16 * 16) and torch.equal(c.room, (c.table >= 0).sum(3).int() * 16)
+    c.reserve(rows.clamp_max(20) + 1)                  # what a head has it keeps
+    assert torch.equal(c.room, (c.table >= 0).sum(3).int() * 16) and (c.room.long() >= (rows + 15) // 16 * 16).all()
+    c.release(0)
+    assert (c.room[:, 0] == 0).all() and torch.equal(c.room[:, 1], (c.table[:, 1] >= 0).sum(2).int() * 16)
+    c.check()
+    c.status.fill_(L.DEV_BOUNDS)
+    with pytest.raises(RuntimeError):
+        c.check()
+    c.check()
+
+
 def test_tree_workspace_is_small(lib):
     """The widest trees over the longest caches fit 32 MiB, a token over a short cache asks for little."""
     for H, Hkv in ((8, 8), (28, 4), (32, 8), (48, 8), (64, 1)):

@@ -634,6 +634,61 @@ def test_drafts_over_a_compressed_cache():
         new.reserve(new.len.cpu() + 4 * page)
 
 
+def test_a_commit_without_pages_is_no_commit():
+    """Sequences whose drafts do not fit the pages that every head of every layer has stay as they were, in all layers; the others
+    are committed, and with pages the rest follows."""
+    from paper_2509_00419_b200 import pipeline as P
+    r = np.random.default_rng(22)
+    nl, B, Hkv, T, page = 2, 3, 2, 5, 16
+    c = P.PagedLayers(nl, B, 4, Hkv, 40, page, 4, T, "cuda")
+    c.K.fill_(float("nan")); c.V.fill_(float("nan"))
+    ln = np.array([[[3, 30], [16, 12], [14, 0]], [[8, 1], [9, 32], [5, 6]]])
+    c.reserve(torch.from_numpy(ln))
+    K, V = (np.zeros((nl, B, Hkv, 64, 128)) for _ in range(2))
+    for l in range(nl):                                              # what the heads hold, by the library's own append
+        for b in range(B):
+            for g in range(Hkv):
+                n = int(ln[l, b, g])
+                if n:
+                    k, v = bf(r, 1, n, 1, 128), bf(r, 1, n, 1, 128)
+                    one = c.len[l, b, g:g + 1].view(1, 1)
+                    L.rope_append(k.cuda(), v.cuda(), None, None, c.K, c.V, one, table=c.table[l, b, g].view(1, 1, -1))
+                    K[l, b, g, :n], V[l, b, g, :n] = f64(k)[0, :, 0], f64(v)[0, :, 0]
+    Kd, Vd = bf(r, nl, B, Hkv, T, 128), bf(r, nl, B, Hkv, T, 128)
+    c.Kd.copy_(Kd); c.Vd.copy_(Vd)
+    index = np.stack([np.sort(r.permutation(T)) for _ in range(B)])
+    count = np.array([2, 4, 2])       # of layer and sequence (0, 1) a head is full, of (1, 1) another; of (0, 2) one is empty and has no page at all
+
+    def compare():
+        lens = i32(c.len)
+        assert np.array_equal(lens, ln)
+        for l in range(nl):
+            lk, lv = f64(logical(c.K, c.table[l].clamp_min(0))), f64(logical(c.V, c.table[l].clamp_min(0)))
+            for b in range(B):
+                for g in range(Hkv):
+                    n = lens[l, b, g]
+                    assert np.array_equal(lk[b, g, :n], K[l, b, g, :n]) and np.array_equal(lv[b, g, :n], V[l, b, g, :n])
+
+    compare()
+    c.check()
+    before = c.K.clone(), c.V.clone()
+    c.commit(dev(index), dev(count))
+    with pytest.raises(RuntimeError):
+        c.check()
+    own = c.table[:, 1:][c.table[:, 1:] >= 0].long()                 # the pages of the sequences that have to wait
+    assert same(c.K[own], before[0][own]) and same(c.V[own], before[1][own])
+    for l in range(nl):
+        K[l], V[l], ln[l] = DO.commit(K[l], V[l], ln[l], f64(Kd[l]), f64(Vd[l]), index, [2, 0, 0])
+    compare()
+    c.check()
+    c.reserve(c.len.cpu() + T)
+    c.commit(dev(index), dev([0, 4, 2]))
+    for l in range(nl):
+        K[l], V[l], ln[l] = DO.commit(K[l], V[l], ln[l], f64(Kd[l]), f64(Vd[l]), index, [0, 4, 2])
+    compare()
+    c.check()
+
+
 @pytest.mark.parametrize("H,Hkv,T,lens", [(8, 2, 3, [700, 33, 5, 129]), (8, 1, 30, [3000, 100]), (2, 2, 200, [300, 40, 0, 511])])
 def test_a_step_in_a_graph(H, Hkv, T, lens):
     """Append, attention and commit captured once and replayed over caches that grow: as the same calls made one by one."""
