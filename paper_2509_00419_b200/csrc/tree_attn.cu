@@ -22,7 +22,7 @@ constexpr int kTreeStageKeys = 64;
 constexpr int kTreeBox = kTreeStageKeys * 128;       // 64 keys x 64 channels
 constexpr int kTreeStageBytes = 4 * kTreeBox;        // K low, K high, V low, V high channels
 constexpr int kTreeMaxCluster = 8;
-constexpr int kTreeMmaWords = 2;                     // mask words of a row: T <= 64
+static_assert(2 * kTreeRows <= 32, "at most 32 rows, so at most 32 drafts: a mask word a row");
 constexpr int kTreePitch = kHeadDim + 4;             // of a row of the results in shared memory
 
 // R groups: two CTAs an SM with a ring of 96 KB each, or one with 192 KB.
@@ -126,13 +126,12 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
     } else {
         uint32_t qa[8][4];
         const uint32_t* qp[2];
-        uint32_t see[2][kTreeMmaWords];                         // draft mask of my two rows
+        uint32_t see[2];                                        // draft mask of my two rows
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int r = gr0 + row + 8 * u, t = r / G, hh = r % G;
             qp[u] = r < rows ? reinterpret_cast<const uint32_t*>(a.q + (int64_t)b * a.q_sb + (int64_t)t * a.q_sn + (int64_t)(g * G + hh) * a.q_sh) : nullptr;
-#pragma unroll
-            for (int w = 0; w < kTreeMmaWords; ++w) see[u][w] = r < rows ? tree_see(a, b, t, n, w) : 0u;
+            see[u] = r < rows ? tree_see(a, b, t, n, 0) : 0u;
         }
 #pragma unroll
         for (int ks = 0; ks < 8; ++ks)
@@ -176,12 +175,7 @@ tree_mma_kernel(const __grid_constant__ CUtensorMap kmap, const __grid_constant_
                     for (int e = 0; e < 4; ++e) {
                         const int j = k0 + 8 * x + 2 * qd + (e & 1), u = e >> 1;
                         bool vis = j < kend;
-                        if (draft) {
-                            uint32_t word = 0;
-#pragma unroll
-                            for (int w = 0; w < kTreeMmaWords; ++w) word = w == (j >> 5) ? see[u][w] : word;
-                            vis = vis && ((word >> (j & 31)) & 1u);
-                        }
+                        if (draft) vis = vis && ((see[u] >> (j & 31)) & 1u);       // (j < kend <= 32 where it counts)
                         sc[x][e] = vis ? sc[x][e] * a.scale_log2 : -INFINITY;
                         tmax[u] = fmaxf(tmax[u], sc[x][e]);
                     }
@@ -475,7 +469,7 @@ static bool tree_layout(const lvlm_dims* d, int64_t cap, TreeLayout* L) {
     const int64_t waves = (heads * S + room - 1) / room, run = (stages + S - 1) / S;
     const double mma_us = R == 1 ? 5 + (heads * S <= kTreeTcCtas ? 1.0 : 1.2) * waves * run : 7 + 1.13 * waves * run;
     const double tc_us = units <= kTreeTcCtas ? 12 + 1.55 * (double)((tc_steps + parts - 1) / parts) * unit_tiles : L->runs ? runs_us : waves_us;
-    L->tc = R > 2 || d->T > 32 * kTreeMmaWords || tc_us < mma_us;
+    L->tc = R > 2 || tc_us < mma_us;
     L->R = R;
     L->S = L->tc ? (int)parts : S;
     L->tiles = tiles;
