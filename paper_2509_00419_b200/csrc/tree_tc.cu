@@ -18,6 +18,8 @@
 // keys 580 us (1080 TFLOP/s, remainders counted).  Short calls: latency; of 16 us (104 rows x 3008 keys) the combining launch is 2.4.
 // Rows of V behind the end of the cache or of the drafts are zeroed in shared memory before they are multiplied: they may hold
 // anything, and their weight of zero would not stop a NaN.
+#include <atomic>
+
 #include "exp2.cuh"
 #include "sm100.cuh"
 #include "tree_attn.cuh"
@@ -604,11 +606,13 @@ template <bool RUNS>
 static lvlm_status launch_tree_tc(const TreeArgs& a, const TreeMaps& m, dim3 ctas, cudaStream_t stream) {
     const size_t smem = 1024 + (size_t)kTTile * (2 + 2 * kTStages) + sizeof(TreeTcSmem);
     LVLM_RETURN_IF_CUDA(cudaFuncSetAttribute(tree_tc_kernel<RUNS>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem));
-    static int regs = 0;                                                   // (looked up once; any thread finds the same)
+    static std::atomic<int> looked_up{0};                                  // (once; any thread finds the same)
+    int regs = looked_up.load(std::memory_order_relaxed);
     if (regs == 0) {
         cudaFuncAttributes f;
         LVLM_RETURN_IF_CUDA(cudaFuncGetAttributes(&f, tree_tc_kernel<RUNS>));
         regs = f.numRegs;
+        looked_up.store(regs, std::memory_order_relaxed);
     }
     if (3 * regs < kTRegsFew + 2 * kTRegsMany) return LVLM_ERR_CUDA;       // the split would wait for registers that nobody has
     return launch_kernel(tree_tc_kernel<RUNS>, ctas, dim3(kTThreads), smem, stream, 1, m.q, m.k, m.v, m.kd, m.vd, a);
