@@ -334,9 +334,10 @@ lvlm_status lvlm_decode_attn_static(const void* q, void* Kc, void* Vc, int32_t* 
  *
  * In all three, `count` (NULL = d->T everywhere) holds the new rows or drafts of each sequence, at most d->T; what
  * belongs to the others is neither read nor written.  A count outside [0, T] is taken as 0 and sets LVLM_DEV_BOUNDS.
- * A head whose len lies outside [0, cap], or an append that does not fit behind it, is skipped: nothing of that head is written,
- * its length stays, and LVLM_DEV_BOUNDS is set.  A page number outside [0, n_pages) sets it too; an append skips that row,
- * lvlm_tree_attn takes zeros for the rows of that page.
+ * A head whose len lies outside [0, cap] sets LVLM_DEV_BOUNDS, and so does an append that does not fit behind it: the two that append
+ * skip it, nothing of that head is written and its length stays; lvlm_tree_attn gives out = 0 and lse = -inf for all of its rows
+ * t < count, whatever drafts they see.  A page number outside [0, n_pages) sets it too; an append skips that row, lvlm_tree_attn takes
+ * zeros for the rows of that page.
  */
 
 /*

@@ -359,7 +359,7 @@ def _refuse(t: torch.Tensor, name: str, dtype, shape, device: int, rows: bool):
     raise ValueError(f"{name} has to be " + ("contiguous in its last dimension" if rows else "contiguous"))
 
 
-# One comparison an argument on the way through: a call of lvlm_rope_append spends 5 us of host time in its launch.
+# One comparison an argument on the way through: of 11 to 13 us of host time a call the C entry takes 3.4 (appends) to 4.3 (attention).
 def _arg(t: Optional[torch.Tensor], name: str, dtype, shape, device: int):
     """Pointer of an optional contiguous argument after the checks that the C call cannot make."""
     if t is None:
@@ -575,7 +575,8 @@ def tree_attn(q, Kc, Vc, length, *, Kd=None, Vd=None, mask=None, count=None, tab
     """lvlm_tree_attn.  q [B,T,H,D] (a view with strides is fine) attends to ``length`` [B,Hkv] rows of a cache and to the
     drafts Kd, Vd [B,Hkv,>=T,D] that ``mask`` lets it see ([B,T,W] or [T,W] int32 words from ``tree_mask``; None = a chain).  count
     [B]: drafts of each sequence (None = T).  max_len: rows a head is expected to hold at most, where the caller knows (it decides
-    how the work is split, not the result).  Returns (out [B,T,H,D], lse [B,H,T] or None); rows behind count are left as they were."""
+    how the work is split, not the result).  out may be q itself where q is contiguous.  Returns (out [B,T,H,D], lse [B,H,T] or None);
+    rows behind count are left as they were."""
     dev = _here(q)
     shape = q.shape
     B, T, H, D = shape

@@ -465,7 +465,8 @@ static bool tree_layout(const lvlm_dims* d, int64_t cap, TreeLayout* L) {
 
     // Estimates in us, fitted to caches of 100 to 33000 keys of 4 to 256 heads (10 % off), from a stage a CTA.  Measured, mma.sync / tcgen05:
     // 16 rows or less, 4 heads x 3008 keys 10.8 / 13.0, x 9000 22 / 17; 16 heads x 9000 26 / 26; 64 heads x 9000 51 / 68; 17 to 32 rows,
-    // 8 heads x 1100 10.2 / 11.5, x 9000 27 / 20, 64 heads x 3008 35 / 33.
+    // 8 heads x 1100 10.2 / 11.5, x 9000 27 / 20, 64 heads x 3008 35 / 33.  The rule is wrong by up to 12 % at 17 to 32 rows of many heads with
+    // short caches: 128 heads x 100 11.7 / 10.6, x 300 15.2 / 13.7, 256 heads x 100 22.4 / 20.1, x 300 29.8 / 26.8 go to mma.sync.
     const int64_t waves = (heads * S + room - 1) / room, run = (stages + S - 1) / S;
     const double mma_us = R == 1 ? 5 + (heads * S <= kTreeTcCtas ? 1.0 : 1.2) * waves * run : 7 + 1.13 * waves * run;
     const double tc_us = units <= kTreeTcCtas ? 12 + 1.55 * (double)((tc_steps + parts - 1) / parts) * unit_tiles : L->runs ? runs_us : waves_us;

@@ -12,10 +12,13 @@
 // - on the device, which alone knows the lengths - and every CTA takes an equal run of them: a scheduler warp cuts the run into segments,
 // a unit each, and the other warps work through them without stopping in between (the keys of the next segment are fetched during
 // the epilogue of this one).
-// A unit that is cut leaves its parts (max, sum, output) in the workspace; tree_combine_kernel adds them in order.
+// A unit that is cut leaves its parts (max, sum, output) in the workspace, in runs one of them half in `out` (TreeArgs);
+// tree_combine_kernel adds them in order.
 // What bounds it: long calls the MMAs, 48 of 128x128x16 a turn of both row tiles, a third of them for the remainders of P.  16 sequences of up to
 // 244 rows x 1888 keys 53 us (tensor pipe active 0.69 of the time on the busiest SM, which includes start and end), 4 of 1536 rows x 16640
-// keys 580 us (1080 TFLOP/s, remainders counted).  Short calls: latency; of 16 us (104 rows x 3008 keys) the combining launch is 2.4.
+// keys 569 to 602 us from one GPU to another (1050 to 1100 TFLOP/s, remainders counted; pipe active 0.67 on every SM).  Short calls:
+// latency; of 16 us (182 rows x 3008 keys) the combining launch is 2.4.  168 registers a thread, the softmax warps' 200 are given later:
+// 12 bytes of a thread spill, 48 in the form with runs.
 // Rows of V behind the end of the cache or of the drafts are zeroed in shared memory before they are multiplied: they may hold
 // anything, and their weight of zero would not stop a NaN.
 #include <atomic>
