@@ -281,7 +281,7 @@ extern "C" lvlm_status lvlm_rope_append(const void* q, const void* k_new, const 
         a.q_sh % 8 || a.q_sn % 8 || a.q_sb % 8 || a.n_sh % 8 || a.n_sn % 8 || a.n_sb % 8)
         return LVLM_ERR_ALIGNMENT;
     if (q && q_out != q &&
-        overlap(q, 2 * ((d->B - 1) * a.q_sb + (d->T - 1) * a.q_sn + (d->H - 1) * a.q_sh + kHeadDim), q_out, 2 * d->B * a.qo_sb))
+        overlap(q, 2 * ((d->B - 1) * a.q_sb + (d->T - 1) * a.q_sn + (d->H - 1) * a.q_sh + kHeadDim), q_out, 2 * (int64_t)d->B * a.qo_sb))
         return LVLM_ERR_INVALID_ARG;
     const int64_t tokens = (int64_t)d->B * d->T, heads = (int64_t)d->B * d->Hkv;
     if (tokens > 0x7FFFFFFFll || heads > 0x7FFFFFFFll) return LVLM_ERR_UNSUPPORTED;

@@ -536,7 +536,7 @@ extern "C" lvlm_status lvlm_tree_attn(const void* q, const void* Kc, const void*
     // Queries may be overwritten where a row's result takes its own query's place; anywhere else CTAs may still have to read them.
     const int64_t packed_n = (int64_t)d->H * d->D, packed_b = d->T * packed_n;
     if (out == q ? (d->H > 1 && a.q_sh != d->D) || (d->T > 1 && a.q_sn != packed_n) || (d->B > 1 && a.q_sb != packed_b)
-                 : overlap(q, 2 * ((d->B - 1) * a.q_sb + (d->T - 1) * a.q_sn + (d->H - 1) * a.q_sh + kHeadDim), out, 2 * d->B * packed_b))
+                 : overlap(q, 2 * ((d->B - 1) * a.q_sb + (d->T - 1) * a.q_sn + (d->H - 1) * a.q_sh + kHeadDim), out, 2 * (int64_t)d->B * packed_b))
         return LVLM_ERR_INVALID_ARG;
     TreeLayout L;
     if (!tree_layout(d, a.c.cap, &L)) return LVLM_ERR_INVALID_ARG;
